@@ -94,6 +94,38 @@ typedef struct prhs_kv {
   int32_t max_seq_len;         /* host-known bound on seq_lens; < 2^22 */
 } prhs_kv;
 
+/* A layer's KV cache held in 8 bits: e4m3 elements (1 sign, 4 exponent, 3
+ * mantissa bits, bias 7, no infinities) and one fp32 scale for each block of
+ * block_size consecutive tokens and kv head.  The element x8 of a block with
+ * scale s stands for s * x8.  kv describes shapes, layout, block table and
+ * lengths as for any cache; kv.k and kv.v point to the e4m3 bytes (written
+ * by prhs_quant_store), and kv.dtype is the type of the queries and of the
+ * keys and values that are stored.  With rows numbered as they lie in memory
+ * (a row: one token of one kv head), row r's scale is entry r / block_size of
+ * k_scale and v_scale: [batch][num_kv_heads][capacity / block_size] for a
+ * contiguous cache, whose capacity is a multiple of block_size, and
+ * [num_pages][num_kv_heads] for a paged one, whose page_size is block_size.
+ * Scales are positive and finite; those prhs_quant_store writes are powers of
+ * two.  16-byte aligned k and v. */
+typedef struct prhs_quant_kv {
+  prhs_kv kv;
+  int32_t block_size;  /* 16, 32, 64 or 128 */
+  float* k_scale;
+  float* v_scale;
+} prhs_quant_kv;
+
+/* Key bounds of the blocks of a cache: for every block of block_size tokens
+ * and kv head the elementwise minimum and maximum of its keys, in the cache's
+ * dtype (for an 8-bit cache the type of its queries), [block][head_dim] with
+ * the blocks numbered as the scales of prhs_quant_kv are (the cache's
+ * capacity is a multiple of block_size, or its page_size is block_size).
+ * 16-byte aligned. */
+typedef struct prhs_bounds {
+  int32_t block_size;  /* 16, 32, 64 or 128 */
+  void* k_min;
+  void* k_max;
+} prhs_bounds;
+
 /* Selection budget and reuse schedule (Sec. 4.1; defaults of Sec. 5.1). */
 typedef struct prhs_params {
   int32_t k;              /* middle budget when k_den == 0 */
@@ -133,7 +165,9 @@ enum {
   PRHS_OP_SELECT = 0,
   PRHS_OP_DILATE_REUSE = 1,
   PRHS_OP_SPARSE_ATTN = 2,
-  PRHS_OP_DENSE_ATTN = 3
+  PRHS_OP_DENSE_ATTN = 3,
+  PRHS_OP_QUANT_SPARSE_ATTN = 4,  /* kv: that of the 8-bit cache */
+  PRHS_OP_QUANT_DENSE_ATTN = 5
 };
 
 enum { PRHS_REUSE = 0, PRHS_REFRESH = 1 };
@@ -164,7 +198,7 @@ int32_t prhs_max_topk(const prhs_params* params, int32_t max_seq_len);
 int32_t prhs_set_capacity(const prhs_params* params, int32_t max_seq_len);
 
 /* Device workspace in bytes that entry point `op` (PRHS_OP_*) needs for this
- * cache shape; set_cap is used by PRHS_OP_SPARSE_ATTN only.  For attention it
+ * cache shape; set_cap is used by the sparse attentions only.  For attention it
  * also holds every call with a smaller batch, set_cap or max_seq_len and the
  * rest the same.  0 bytes is a valid answer (ws may then be NULL). */
 prhs_status prhs_workspace_size(int32_t op, const prhs_kv* kv, const prhs_params* params,
@@ -441,6 +475,117 @@ prhs_status prhs_pool_decode_attn(const prhs_kv* kv, const void* q, const int32_
                                   const int32_t* unit_gate, int32_t units_side,
                                   const prhs_psaw* psaw, float scale, float* out, float* lse,
                                   void* ws, size_t ws_bytes, void* stream);
+
+/* ---- 8-bit KV cache ----------------------------------------------------------
+ *
+ * prhs_quant_store writes tokens into it, the prhs_quant_*_decode_attn calls
+ * attend it as their namesakes attend a bf16 or fp32 cache. */
+
+/* Stores new keys and values.  For every sequence b with n = seq_lens[b] and
+ * c = min(new_lens[b], new_cap, n) (new_lens NULL: c = min(new_cap, n)), the
+ * first c tokens of k_new[b] and v_new[b] go to positions [n - c, n): the
+ * lengths count the new tokens.  Positions below n - c hold what was stored
+ * before; rows at and behind n are left as they are.
+ * For each block of each kv head that gets a token, K and V apart:
+ *   s_new = 2^e, e the smallest integer >= -100 with amax <= 448 * 2^e, amax
+ *     the largest finite |x| among the block's new tokens;
+ *   s = s_new where the block holds no earlier token, else max(s_old, s_new);
+ *   new elements are rounded to the nearest e4m3 value of x / s (ties to
+ *     even); where s > s_old, the block's earlier elements are rounded again
+ *     likewise, from s_old * x8 / s (exact but for values that fall below
+ *     2^-6 s: both scales are powers of two where this call wrote them).
+ * NaN and infinite elements become NaN.
+ * bounds (may be NULL; its block_size that of kv): the key bounds of these
+ * blocks, from the new tokens' keys as given, NaN left out, and, where the
+ * block holds earlier tokens, from its present bounds.
+ * k_new, v_new: [batch][num_kv_heads][new_cap][head_dim] in kv->kv.dtype;
+ * new_lens: [batch] int32 device array or NULL.
+ * Two sequences whose block tables name one page must not both store into it
+ * in one call (its contents are then unspecified).  Tokens on pages outside
+ * the pool are dropped.  No workspace. */
+prhs_status prhs_quant_store(const prhs_quant_kv* kv, const void* k_new, const void* v_new,
+                             int32_t new_cap, const int32_t* new_lens, const prhs_bounds* bounds,
+                             void* stream);
+
+/* prhs_sparse_decode_attn, prhs_reuse_decode_attn, prhs_dense_decode_attn and
+ * prhs_pool_decode_attn over an 8-bit cache: same arguments, semantics and
+ * outputs, with k_i = k_scale * k8_i and v_i = v_scale * v8_i of the block of
+ * token i.  Products are accumulated in fp32 and weights keep 22 bits.
+ * ws: >= prhs_workspace_size(PRHS_OP_QUANT_SPARSE_ATTN, set_cap) bytes, for
+ * the dense form PRHS_OP_QUANT_DENSE_ATTN; no initialisation needed. */
+prhs_status prhs_quant_sparse_decode_attn(const prhs_quant_kv* kv, const void* q,
+                                          const int32_t* set_idx, const int32_t* set_len,
+                                          int32_t set_cap, float scale, float* out, float* lse,
+                                          void* ws, size_t ws_bytes, void* stream);
+prhs_status prhs_quant_reuse_decode_attn(const prhs_quant_kv* kv, const void* q,
+                                         const int32_t* set_idx, const int32_t* set_len,
+                                         int32_t set_cap, const int32_t* anchor_lens, float scale,
+                                         float* out, float* lse, void* ws, size_t ws_bytes,
+                                         void* stream);
+prhs_status prhs_quant_dense_decode_attn(const prhs_quant_kv* kv, const void* q, float scale,
+                                         float* out, float* lse, void* ws, size_t ws_bytes,
+                                         void* stream);
+prhs_status prhs_quant_pool_decode_attn(const prhs_quant_kv* kv, const void* q,
+                                        const int32_t* pool_idx, const int32_t* pool_len,
+                                        int32_t pool_rows, int32_t set_cap,
+                                        const int32_t* unit_row, const int32_t* unit_tail,
+                                        const int32_t* unit_gate, int32_t units_side,
+                                        const prhs_psaw* psaw, float scale, float* out, float* lse,
+                                        void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Selection of whole blocks by their key bounds ---------------------------- */
+
+/* Key bounds of a bf16 or fp32 cache, for the blocks that hold a position of
+ * [n - c, n) with n and c as in prhs_quant_store: elementwise minimum and
+ * maximum of the block's keys at positions below n, NaN left out.  Call it
+ * after the new keys are in the cache; with c = n it makes all bounds anew.
+ * Blocks on pages outside the pool are left out.  No workspace. */
+prhs_status prhs_block_bounds(const prhs_kv* kv, const prhs_bounds* bounds, int32_t new_cap,
+                              const int32_t* new_lens, void* stream);
+
+/* Most blocks that prhs_block_select takes for a row of at most max_seq_len
+ * tokens: the minimum blk_cap.  -1 on bad arguments. */
+int32_t prhs_max_blocks(const prhs_params* params, int32_t block_size, int32_t max_seq_len);
+
+/* Smallest set_cap that holds every set of prhs_block_select and, through
+ * prhs_*_reuse_decode_attn, the tokens decoded in its refresh period:
+ * min(max_seq_len, sink + prhs_max_blocks() * block_size + window +
+ * refresh_every - 1).  -1 on bad arguments. */
+int32_t prhs_block_set_capacity(const prhs_params* params, int32_t block_size,
+                                int32_t max_seq_len);
+
+/* Device workspace in bytes of prhs_block_select for this cache shape (also
+ * for smaller batches and lengths). */
+prhs_status prhs_block_workspace_size(const prhs_kv* kv, const prhs_bounds* bounds, size_t* bytes);
+
+/* Selection of whole blocks: an alternative to prhs_select that reads the
+ * blocks' bounds instead of every key.  For every (b, kv head g) with
+ * n0 = seq_lens[b], middle range [sink', win) = [min(sink, n0),
+ * max(sink', n0 - window)) and budget k_b of prhs_params (tokens):
+ *   the candidates are the blocks that hold a position of the middle range;
+ *   sigma_j = max over the group's query heads h of
+ *     sum_d max(q[b][h][d] k_min[j][d], q[b][h][d] k_max[j][d])  (fp32),
+ *     which no key of block j exceeds in q . k;
+ *   the min(ceil(k_b / block_size), candidates) blocks of largest sigma are
+ *   chosen, ties going to the lower block;
+ *   blk_idx[b][g][0 .. blk_len) = the chosen blocks, ascending;
+ *   set_idx[b][g][0 .. set_len) = [0, sink') U the chosen blocks' positions
+ *     below n0 U [win, n0), ascending and without duplicates: a set for any
+ *     of the sparse and reuse attention calls.
+ * kv: shapes, layout, block table and lengths (for an 8-bit cache its kv);
+ * its k and v are not read.  params: k, k_num, k_den, sink and window count.
+ * blk_idx: [batch][num_kv_heads][blk_cap] int32, blk_cap >=
+ * prhs_max_blocks(); blk_len [batch][num_kv_heads]; set_idx:
+ * [batch][num_kv_heads][set_cap], set_cap >= min(max_seq_len, sink +
+ * prhs_max_blocks() * block_size + window); set_len [batch][num_kv_heads].
+ * Entries behind the lengths are left as they are.
+ * ws: >= prhs_block_workspace_size() bytes, no initialisation needed.
+ * NaN scores and blocks on pages outside the pool rank last.  -0.0 ranks
+ * equal to +0.0. */
+prhs_status prhs_block_select(const prhs_kv* kv, const void* q, const prhs_params* params,
+                              const prhs_bounds* bounds, int32_t* blk_idx, int32_t* blk_len,
+                              int32_t blk_cap, int32_t* set_idx, int32_t* set_len,
+                              int32_t set_cap, void* ws, size_t ws_bytes, void* stream);
 
 /* Message for the last non-OK status returned on the calling thread. */
 const char* prhs_last_error(void);

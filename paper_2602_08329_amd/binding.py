@@ -43,6 +43,8 @@ PRHS_OP_SELECT = 0
 PRHS_OP_DILATE_REUSE = 1
 PRHS_OP_SPARSE_ATTN = 2
 PRHS_OP_DENSE_ATTN = 3
+PRHS_OP_QUANT_SPARSE_ATTN = 4
+PRHS_OP_QUANT_DENSE_ATTN = 5
 
 PRHS_REUSE = 0
 PRHS_REFRESH = 1
@@ -58,6 +60,9 @@ EXPORTS = [
     "prhs_reuse_decode_attn", "prhs_dense_decode_attn", "prhs_gate", "prhs_gate_select",
     "prhs_select_gated",
     "prhs_pool_decode_attn", "prhs_prefill_attn", "prhs_psaw_first_visible", "prhs_last_error",
+    "prhs_quant_store", "prhs_quant_sparse_decode_attn", "prhs_quant_reuse_decode_attn",
+    "prhs_quant_dense_decode_attn", "prhs_quant_pool_decode_attn", "prhs_block_bounds",
+    "prhs_max_blocks", "prhs_block_set_capacity", "prhs_block_workspace_size", "prhs_block_select",
 ]
 
 
@@ -87,6 +92,19 @@ class PrhsPsaw(ctypes.Structure):
     _fields_ = [
         ("layer", ctypes.c_int32), ("num_layers", ctypes.c_int32), ("l_s", ctypes.c_int32),
         ("sink", ctypes.c_int32), ("phi", ctypes.c_double), ("alpha", ctypes.c_double),
+    ]
+
+
+class PrhsQuantKv(ctypes.Structure):
+    _fields_ = [
+        ("kv", PrhsKv), ("block_size", ctypes.c_int32),
+        ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class PrhsBounds(ctypes.Structure):
+    _fields_ = [
+        ("block_size", ctypes.c_int32), ("k_min", ctypes.c_void_p), ("k_max", ctypes.c_void_p),
     ]
 
 
@@ -181,6 +199,29 @@ def lib():
         L.prhs_prefill_attn.argtypes = [P(PrhsKv), vp, i32, P(PrhsPsaw), ctypes.c_float, vp, vp, vp]
         L.prhs_psaw_first_visible.restype = i32
         L.prhs_psaw_first_visible.argtypes = [P(PrhsPsaw), i32]
+        Q, Bn, f32 = P(PrhsQuantKv), P(PrhsBounds), ctypes.c_float
+        L.prhs_quant_store.restype = i32
+        L.prhs_quant_store.argtypes = [Q, vp, vp, i32, vp, Bn, vp]
+        L.prhs_quant_sparse_decode_attn.restype = i32
+        L.prhs_quant_sparse_decode_attn.argtypes = [Q, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp]
+        L.prhs_quant_reuse_decode_attn.restype = i32
+        L.prhs_quant_reuse_decode_attn.argtypes = [Q, vp, vp, vp, i32, vp, f32, vp, vp, vp, sz, vp]
+        L.prhs_quant_dense_decode_attn.restype = i32
+        L.prhs_quant_dense_decode_attn.argtypes = [Q, vp, f32, vp, vp, vp, sz, vp]
+        L.prhs_quant_pool_decode_attn.restype = i32
+        L.prhs_quant_pool_decode_attn.argtypes = [Q, vp, vp, vp, i32, i32, vp, vp, vp, i32,
+                                                  P(PrhsPsaw), f32, vp, vp, vp, sz, vp]
+        L.prhs_block_bounds.restype = i32
+        L.prhs_block_bounds.argtypes = [P(PrhsKv), Bn, i32, vp, vp]
+        L.prhs_max_blocks.restype = i32
+        L.prhs_max_blocks.argtypes = [P(PrhsParams), i32, i32]
+        L.prhs_block_set_capacity.restype = i32
+        L.prhs_block_set_capacity.argtypes = [P(PrhsParams), i32, i32]
+        L.prhs_block_workspace_size.restype = i32
+        L.prhs_block_workspace_size.argtypes = [P(PrhsKv), Bn, P(sz)]
+        L.prhs_block_select.restype = i32
+        L.prhs_block_select.argtypes = [P(PrhsKv), vp, P(PrhsParams), Bn, vp, vp, i32, vp, vp, i32,
+                                        vp, sz, vp]
         L.prhs_last_error.restype = ctypes.c_char_p
         L.prhs_last_error.argtypes = []
         _host = _load_host(L)
@@ -314,6 +355,122 @@ class KV:
                   self.c.num_q_heads, table)
 
 
+class QuantKV:
+    """A layer's KV cache in 8 bits: e4m3 tensors K8, V8, contiguous
+    [B][Hkv][capacity][d] or paged [P][Hkv][ps][d] with block_table
+    [B][max_pages] int32, and fp32 scales, one per block of tokens and kv head:
+    contiguous [B][Hkv][capacity / block_size], paged (block_size = ps)
+    [P][Hkv].  dtype is that of the queries and of the keys and values that are
+    stored, bfloat16 or float32.  Holds references to the tensors it points to;
+    prhs_quant_store writes K8, V8 and the scales."""
+
+    def __init__(self, K8, V8, k_scale, v_scale, seq_lens, max_seq_len, num_q_heads,
+                 block_table=None, dtype=torch.bfloat16):
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("dtype must be float32 or bfloat16")
+        _need(K8, torch.float8_e4m3fn, "K8", dims=4)
+        _need(V8, torch.float8_e4m3fn, "V8", shape=K8.shape)
+        _need(k_scale, torch.float32, "k_scale")
+        _need(v_scale, torch.float32, "v_scale", shape=k_scale.shape)
+        _need(seq_lens, torch.int32, "seq_lens", dims=1)
+        if block_table is not None:
+            _need(block_table, torch.int32, "block_table", dims=2)
+        lead, Hkv, rows, d = K8.shape
+        bs = _block_size(k_scale, "k_scale", lead, Hkv, rows, block_table is not None)
+        dt = PRHS_F32 if dtype == torch.float32 else PRHS_BF16
+        if block_table is None:
+            shape = (lead, num_q_heads, Hkv, d, dt, PRHS_KV_CONTIGUOUS, rows, 0, 0, 0)
+            table = None
+        else:
+            shape = (block_table.shape[0], num_q_heads, Hkv, d, dt, PRHS_KV_PAGED, 0, rows,
+                     block_table.shape[1], lead)
+            table = block_table.data_ptr()
+        self.quant = PrhsQuantKv(PrhsKv(*shape, K8.data_ptr(), V8.data_ptr(), table,
+                                        seq_lens.data_ptr(), max_seq_len),
+                                 bs, k_scale.data_ptr(), v_scale.data_ptr())
+        self.shape_c = self.quant.kv    # shapes, table and lengths: not a cache of its own
+        if seq_lens.numel() != self.shape_c.batch:
+            raise ValueError("seq_lens must have one entry per sequence")
+        self._keep = (K8, V8, k_scale, v_scale, seq_lens, block_table)
+        self.dtype = dtype
+        self.device = K8.device
+        self.block_size = bs
+
+    @property
+    def c(self):
+        raise TypeError("an 8-bit cache goes to the prhs_quant_* and prhs_block_select calls")
+
+    def q_shape(self):
+        return (self.shape_c.batch, self.shape_c.num_q_heads, self.shape_c.head_dim)
+
+    def per_unit(self, last=None):
+        base = (self.shape_c.batch, self.shape_c.num_kv_heads)
+        return base if last is None else base + (last,)
+
+    def check_device(self, **tensors):
+        K8, V8, ks, vs, seq_lens, table = self._keep
+        _on_device(self.device, K8=K8, V8=V8, k_scale=ks, v_scale=vs, seq_lens=seq_lens,
+                   block_table=table, **tensors)
+
+    def with_seq_lens(self, seq_lens, max_seq_len=None):
+        """Same cache, other lengths (a new descriptor)."""
+        K8, V8, ks, vs, _, table = self._keep
+        return QuantKV(K8, V8, ks, vs, seq_lens,
+                       self.shape_c.max_seq_len if max_seq_len is None else max_seq_len,
+                       self.shape_c.num_q_heads, table, self.dtype)
+
+
+def _block_size(t, name, lead, Hkv, rows, paged):
+    """Tokens per entry of a tensor with an entry per block and kv head, from
+    its leading dimensions."""
+    if paged:
+        if tuple(t.shape[:2]) != (lead, Hkv):
+            raise ValueError(f"{name} must begin with dims {(lead, Hkv)}, got {tuple(t.shape)}")
+        return rows
+    if t.dim() < 3 or tuple(t.shape[:2]) != (lead, Hkv) or t.shape[2] < 1 or rows % t.shape[2]:
+        raise ValueError(f"{name} must begin with dims ({lead}, {Hkv}, {rows} / block_size), "
+                         f"got {tuple(t.shape)}")
+    return rows // t.shape[2]
+
+
+class BlockBounds:
+    """Key bounds of a cache's blocks (kv: a KV or a QuantKV): k_min and k_max in
+    kv.dtype, contiguous [B][Hkv][capacity / block_size][d], paged [P][Hkv][d]
+    with block_size the page size."""
+
+    def __init__(self, kv, k_min, k_max):
+        c = _shape_of(kv)
+        paged = c.layout == PRHS_KV_PAGED
+        _need(k_min, kv.dtype, "k_min", dims=3 if paged else 4)
+        _need(k_max, kv.dtype, "k_max", shape=k_min.shape)
+        bs = _block_size(k_min, "k_min", c.num_pages if paged else c.batch, c.num_kv_heads,
+                         c.page_size if paged else c.capacity, paged)
+        if k_min.shape[-1] != c.head_dim:
+            raise ValueError(f"k_min must end with dim {c.head_dim}, got {tuple(k_min.shape)}")
+        self._keep = (k_min, k_max)
+        self._of = _geometry(c)
+        self.bounds = PrhsBounds(bs, k_min.data_ptr(), k_max.data_ptr())
+        self.block_size = bs
+
+
+def _shape_of(kv):
+    """The shape descriptor of a KV or a QuantKV."""
+    return kv.shape_c if isinstance(kv, QuantKV) else kv.c
+
+
+def _geometry(c):
+    """What the bounds of a cache depend on."""
+    return (c.layout, c.num_kv_heads, c.head_dim, c.dtype) + (
+        (c.page_size, c.num_pages) if c.layout == PRHS_KV_PAGED else (c.batch, c.capacity))
+
+
+def _fits(kv, bounds):
+    if not isinstance(bounds, BlockBounds):
+        raise TypeError("bounds must be a BlockBounds")
+    if bounds._of != _geometry(_shape_of(kv)):
+        raise ValueError("bounds were made for a cache of another shape")
+
+
 def prhs_max_topk(p, max_seq_len):
     return lib().prhs_max_topk(ctypes.byref(p), max_seq_len)
 
@@ -332,7 +489,7 @@ def prhs_schedule(step, layer, p):
 
 def prhs_workspace_size(op, kv=None, p=None, set_cap=0):
     n = ctypes.c_size_t(0)
-    check(lib().prhs_workspace_size(op, None if kv is None else ctypes.byref(kv.c),
+    check(lib().prhs_workspace_size(op, None if kv is None else ctypes.byref(_shape_of(kv)),
                                     None if p is None else ctypes.byref(p), set_cap,
                                     ctypes.byref(n)))
     return n.value
@@ -356,7 +513,9 @@ def select_zero_bytes(kv):
     return 2 * a256(rows * 8192) + a256(rows * 16)
 
 
-def _q(kv, q):
+def _q(kv, q, kinds=KV):
+    if not isinstance(kv, kinds):
+        raise TypeError("this call does not take a " + type(kv).__name__)
     _need(q, kv.dtype, "q", shape=kv.q_shape())
 
 
@@ -668,3 +827,154 @@ def prhs_dense_decode_attn(kv, q, scale, out, lse, ws, stream=None):
     kv.check_device(q=q, out=out, lse=lse, ws=ws)
     check(lib().prhs_dense_decode_attn(ctypes.byref(kv.c), _ptr(q), float(scale), _ptr(out),
                                        _ptr(lse), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+# ---- 8-bit cache and selection of blocks ----------------------------------------
+
+def _launch(kv, stream, entry, *args):
+    """The library call entry(*args, stream) on the cache's GPU and its current
+    stream, or on `stream`, which has to be one of that GPU."""
+    if stream is None:
+        stream = torch.cuda.current_stream(kv.device)
+    elif stream.device != kv.device:
+        raise ValueError(f"stream is on {stream.device}, the cache on {kv.device}")
+    with torch.cuda.device(kv.device):
+        check(entry(*args, ctypes.c_void_p(stream.cuda_stream)))
+
+
+def _new_lens(kv, new_lens):
+    if new_lens is not None:
+        _need(new_lens, torch.int32, "new_lens", shape=(_shape_of(kv).batch,))
+
+
+def _quant(kv):
+    if not isinstance(kv, QuantKV):
+        raise TypeError("kv must be a QuantKV")
+
+
+def prhs_quant_store(kv, k_new, v_new, new_lens=None, bounds=None, stream=None):
+    """Stores the tokens k_new, v_new [B][Hkv][T][d] (kv.dtype) as the last
+    new_lens[b] (all T by default) of the seq_lens[b] tokens of each sequence of
+    the QuantKV kv, and updates the BlockBounds `bounds` of their blocks."""
+    _quant(kv)
+    _need(k_new, kv.dtype, "k_new", dims=4)
+    _need(k_new, kv.dtype, "k_new", shape=kv.per_unit() + (k_new.shape[2], kv.shape_c.head_dim))
+    _need(v_new, kv.dtype, "v_new", shape=k_new.shape)
+    _new_lens(kv, new_lens)
+    k_min = k_max = None
+    if bounds is not None:
+        _fits(kv, bounds)
+        k_min, k_max = bounds._keep
+    kv.check_device(k_new=k_new, v_new=v_new, new_lens=new_lens, k_min=k_min, k_max=k_max)
+    _launch(kv, stream, lib().prhs_quant_store, ctypes.byref(kv.quant), _ptr(k_new), _ptr(v_new),
+            k_new.shape[2], _ptr(new_lens), None if bounds is None else ctypes.byref(bounds.bounds))
+
+
+def _quant_attention(kv, q, out, lse, ws):
+    _q(kv, q, QuantKV)
+    _outputs(kv, out, lse)
+    _ws(ws)
+
+
+def prhs_quant_sparse_decode_attn(kv, q, set_idx, set_len, scale, out, lse, ws, stream=None):
+    """prhs_sparse_decode_attn over a QuantKV."""
+    _quant_attention(kv, q, out, lse, ws)
+    _sets(kv, set_idx, set_len)
+    kv.check_device(q=q, set_idx=set_idx, set_len=set_len, out=out, lse=lse, ws=ws)
+    _launch(kv, stream, lib().prhs_quant_sparse_decode_attn, ctypes.byref(kv.quant), _ptr(q),
+            _ptr(set_idx), _ptr(set_len), set_idx.shape[-1], float(scale), _ptr(out), _ptr(lse),
+            _ptr(ws), ws.numel())
+
+
+def prhs_quant_reuse_decode_attn(kv, q, set_idx, set_len, anchor_lens, scale, out, lse, ws,
+                                 stream=None):
+    """prhs_reuse_decode_attn over a QuantKV."""
+    _quant_attention(kv, q, out, lse, ws)
+    _sets(kv, set_idx, set_len)
+    _need(anchor_lens, torch.int32, "anchor_lens", shape=(kv.shape_c.batch,))
+    kv.check_device(q=q, set_idx=set_idx, set_len=set_len, anchor_lens=anchor_lens, out=out,
+                    lse=lse, ws=ws)
+    _launch(kv, stream, lib().prhs_quant_reuse_decode_attn, ctypes.byref(kv.quant), _ptr(q),
+            _ptr(set_idx), _ptr(set_len), set_idx.shape[-1], _ptr(anchor_lens), float(scale),
+            _ptr(out), _ptr(lse), _ptr(ws), ws.numel())
+
+
+def prhs_quant_dense_decode_attn(kv, q, scale, out, lse, ws, stream=None):
+    """prhs_dense_decode_attn over a QuantKV."""
+    _quant_attention(kv, q, out, lse, ws)
+    kv.check_device(q=q, out=out, lse=lse, ws=ws)
+    _launch(kv, stream, lib().prhs_quant_dense_decode_attn, ctypes.byref(kv.quant), _ptr(q),
+            float(scale), _ptr(out), _ptr(lse), _ptr(ws), ws.numel())
+
+
+def prhs_quant_pool_decode_attn(kv, q, pool_idx, pool_len, unit_row, unit_tail, scale, out, lse, ws,
+                                stream=None, psaw=None, unit_gate=None, units_side=PRHS_UNITS_ALL):
+    """prhs_pool_decode_attn over a QuantKV."""
+    _quant_attention(kv, q, out, lse, ws)
+    units = kv.shape_c.batch * kv.shape_c.num_kv_heads
+    if units_side != PRHS_UNITS_ALL:
+        _need(unit_gate, torch.int32, "unit_gate", shape=(units,))
+    _need(pool_idx, torch.int32, "pool_idx")
+    if pool_idx.dim() < 1:
+        raise ValueError("pool_idx must have at least one dimension")
+    cap = pool_idx.shape[-1]
+    rows = pool_idx.numel() // max(cap, 1)
+    _need(pool_len, torch.int32, "pool_len", shape=pool_idx.shape[:-1])
+    _need(unit_row, torch.int32, "unit_row", shape=(units,))
+    _need(unit_tail, torch.int32, "unit_tail", shape=(units,))
+    if psaw is not None and not isinstance(psaw, PrhsPsaw):
+        raise TypeError("psaw must be a PrhsPsaw (binding.psaw(...))")
+    kv.check_device(q=q, pool_idx=pool_idx, pool_len=pool_len, unit_row=unit_row,
+                    unit_tail=unit_tail, unit_gate=unit_gate, out=out, lse=lse, ws=ws)
+    _launch(kv, stream, lib().prhs_quant_pool_decode_attn, ctypes.byref(kv.quant), _ptr(q),
+            _ptr(pool_idx), _ptr(pool_len), rows, cap, _ptr(unit_row), _ptr(unit_tail),
+            _ptr(unit_gate) if units_side != PRHS_UNITS_ALL else None, int(units_side), _ref(psaw),
+            float(scale), _ptr(out), _ptr(lse), _ptr(ws), ws.numel())
+
+
+def prhs_block_bounds(kv, bounds, new_cap, new_lens=None, stream=None):
+    """Makes the BlockBounds `bounds` of the KV kv anew for the blocks that hold
+    one of the last new_lens[b] (at most, and by default, new_cap) tokens of
+    each sequence."""
+    if not isinstance(kv, KV):
+        raise TypeError("kv must be a KV (prhs_quant_store keeps the bounds of a QuantKV)")
+    _fits(kv, bounds)
+    _new_lens(kv, new_lens)
+    kv.check_device(k_min=bounds._keep[0], k_max=bounds._keep[1], new_lens=new_lens)
+    _launch(kv, stream, lib().prhs_block_bounds, ctypes.byref(kv.c), ctypes.byref(bounds.bounds),
+            int(new_cap), _ptr(new_lens))
+
+
+def prhs_max_blocks(p, block_size, max_seq_len):
+    return lib().prhs_max_blocks(ctypes.byref(p), block_size, max_seq_len)
+
+
+def prhs_block_set_capacity(p, block_size, max_seq_len):
+    return lib().prhs_block_set_capacity(ctypes.byref(p), block_size, max_seq_len)
+
+
+def prhs_block_workspace_size(kv, bounds):
+    n = ctypes.c_size_t(0)
+    check(lib().prhs_block_workspace_size(ctypes.byref(_shape_of(kv)), ctypes.byref(bounds.bounds),
+                                          ctypes.byref(n)))
+    return n.value
+
+
+def prhs_block_select(kv, q, p, bounds, blk_idx, blk_len, set_idx, set_len, ws, stream=None):
+    """Chooses the blocks of largest key bound for every sequence and kv head of
+    a KV or QuantKV, within the budget and around the sink and window of the
+    params p: their indices blk_idx [B][Hkv][cap], and the set of sink, blocks
+    and window for the attention calls."""
+    _q(kv, q, (KV, QuantKV))
+    _fits(kv, bounds)
+    _need(blk_idx, torch.int32, "blk_idx", dims=3)
+    _need(blk_idx, torch.int32, "blk_idx", shape=kv.per_unit(blk_idx.shape[-1]))
+    _need(blk_len, torch.int32, "blk_len", shape=kv.per_unit())
+    _sets(kv, set_idx, set_len)
+    _ws(ws)
+    kv.check_device(q=q, k_min=bounds._keep[0], k_max=bounds._keep[1], blk_idx=blk_idx,
+                    blk_len=blk_len, set_idx=set_idx, set_len=set_len, ws=ws)
+    _launch(kv, stream, lib().prhs_block_select, ctypes.byref(_shape_of(kv)), _ptr(q),
+            ctypes.byref(p), ctypes.byref(bounds.bounds), _ptr(blk_idx), _ptr(blk_len),
+            blk_idx.shape[-1], _ptr(set_idx), _ptr(set_len), set_idx.shape[-1], _ptr(ws),
+            ws.numel())

@@ -28,7 +28,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libprhs.so")
-SOURCES = ["prhs_api.hip", "select.hip", "dilate.hip", "attention.hip", "gate.hip", "prefill.hip"]
+SOURCES = ["prhs_api.hip", "select.hip", "dilate.hip", "attention.hip", "gate.hip", "prefill.hip",
+           "quant.hip", "quant_attention.hip", "block_select.hip"]
 
 HOST_SOURCE = "host_binding.cpp"
 # with the interpreter's ABI tag, so that another Python does not load it

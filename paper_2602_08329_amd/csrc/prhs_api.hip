@@ -6,6 +6,8 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "prhs.h"
 #include "prhs_internal.h"
 
@@ -84,6 +86,52 @@ prhs_status check_kv_data(const prhs_kv* kv) {
     return fail(PRHS_E_INVALID, "block_table is NULL for a paged cache");
   return PRHS_OK;
 }
+
+// log2 of a block size that fits the cache's layout.
+prhs_status check_blocks(const prhs_kv* kv, int32_t block_size, int* shift) {
+  if (block_size != 16 && block_size != 32 && block_size != 64 && block_size != 128)
+    return fail(PRHS_E_UNSUPPORTED, "block_size must be 16, 32, 64 or 128 (got %d)", block_size);
+  if (kv->layout == PRHS_KV_PAGED ? kv->page_size != block_size : kv->capacity % block_size != 0)
+    return fail(PRHS_E_INVALID, "block_size (%d) must be the page size, or divide the capacity",
+                block_size);
+  *shift = __builtin_ctz((unsigned)block_size);
+  return PRHS_OK;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Workgroups of a launch: its threads, at most 1024 each, must stay countable
+// in 32 bits.
+prhs_status check_grid(long long groups) {
+  if (groups >= (1LL << 22))
+    return fail(PRHS_E_UNSUPPORTED, "the call would launch %lld workgroups, at most 2^22 - 1 are",
+                groups);
+  return PRHS_OK;
+}
+
+prhs_status check_quant_kv(const prhs_quant_kv* kv, int* shift) {
+  if (!kv) return fail(PRHS_E_INVALID, "kv is NULL");
+  prhs_status st = check_kv_shape(&kv->kv);
+  if (st != PRHS_OK) return st;
+  if ((st = check_blocks(&kv->kv, kv->block_size, shift)) != PRHS_OK) return st;
+  if ((st = check_kv_data(&kv->kv)) != PRHS_OK || kv->kv.batch == 0) return st;
+  if (!kv->k_scale || !kv->v_scale) return fail(PRHS_E_INVALID, "k_scale or v_scale is NULL");
+  if (!aligned16(kv->kv.k) || !aligned16(kv->kv.v))
+    return fail(PRHS_E_INVALID, "k and v must be 16-byte aligned");
+  return PRHS_OK;
+}
+
+prhs_status check_bounds(const prhs_kv* kv, const prhs_bounds* bounds, int* shift) {
+  if (!bounds) return fail(PRHS_E_INVALID, "bounds is NULL");
+  prhs_status st = check_blocks(kv, bounds->block_size, shift);
+  if (st != PRHS_OK || kv->batch == 0) return st;
+  if (!bounds->k_min || !bounds->k_max) return fail(PRHS_E_INVALID, "k_min or k_max is NULL");
+  if (!aligned16(bounds->k_min) || !aligned16(bounds->k_max))
+    return fail(PRHS_E_INVALID, "k_min and k_max must be 16-byte aligned");
+  return PRHS_OK;
+}
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 prhs::KvView view_of(const prhs_kv* kv) {
   prhs::KvView v;
@@ -215,6 +263,16 @@ prhs_status prhs_workspace_size(int32_t op, const prhs_kv* kv, const prhs_params
                                           kv->num_kv_heads, kv->head_dim, kv->max_seq_len);
       return PRHS_OK;
     }
+    case PRHS_OP_QUANT_SPARSE_ATTN:
+    case PRHS_OP_QUANT_DENSE_ATTN: {
+      prhs_status st = check_kv_shape(kv);
+      if (st != PRHS_OK) return st;
+      const bool dense = op == PRHS_OP_QUANT_DENSE_ATTN;
+      if (!dense && set_cap < 0) return fail(PRHS_E_INVALID, "set_cap must be >= 0");
+      *bytes = prhs::quant_attn_workspace_bytes(dense, kv->batch, kv->num_q_heads, kv->num_kv_heads,
+                                                kv->head_dim, dense ? kv->max_seq_len : set_cap);
+      return PRHS_OK;
+    }
     default:
       return fail(PRHS_E_INVALID, "unknown op %d", op);
   }
@@ -337,7 +395,8 @@ prhs_status prhs_dilate_reuse(const prhs_params* params, int32_t batch, int32_t 
   return device_status(prhs::launch_dilate_reuse(a, (hipStream_t)stream), "prhs_dilate_reuse launch");
 }
 
-static prhs_status attention_common(const prhs_kv* kv, const void* q, const int32_t* set_idx,
+static prhs_status attention_common(const prhs_kv* kv, const prhs::QuantScales* scales,
+                                    const void* q, const int32_t* set_idx,
                                     const int32_t* set_len, int32_t set_cap,
                                     const int32_t* tail_start, const int32_t* unit_row,
                                     const int32_t* unit_tail, int32_t pool_rows,
@@ -358,8 +417,15 @@ static prhs_status attention_common(const prhs_kv* kv, const void* q, const int3
   double psaw_f = 0.0;
   if (psaw && (st = psaw_factor(psaw, &psaw_f)) != PRHS_OK) return st;
   const int rows_cap = dense ? kv->max_seq_len : set_cap;
-  const size_t wsz = prhs::attn_call_bytes(kv->dtype, dense, kv->batch, kv->num_q_heads,
-                                           kv->num_kv_heads, kv->head_dim, rows_cap);
+  if (scales && (st = check_grid(std::max((long long)kv->batch * kv->num_q_heads,
+                                          prhs::quant_attn_groups(dense, kv->batch, kv->num_kv_heads,
+                                                                  rows_cap)))) != PRHS_OK)
+    return st;
+  const size_t wsz =
+      scales ? prhs::quant_attn_call_bytes(dense, kv->batch, kv->num_q_heads, kv->num_kv_heads,
+                                           kv->head_dim, rows_cap)
+             : prhs::attn_call_bytes(kv->dtype, dense, kv->batch, kv->num_q_heads,
+                                     kv->num_kv_heads, kv->head_dim, rows_cap);
   if (kv->batch > 0 && (!ws || ws_bytes < wsz))
     return fail(PRHS_E_WORKSPACE, "workspace of %zu bytes needed (got %zu)", wsz, ws_bytes);
   if (kv->batch == 0) return PRHS_OK;
@@ -383,14 +449,16 @@ static prhs_status attention_common(const prhs_kv* kv, const void* q, const int3
   a.out = out;
   a.lse = lse;
   a.ws = ws;
-  return device_status(prhs::launch_attention(a, dense, (hipStream_t)stream), name);
+  return device_status(scales ? prhs::launch_quant_attention(a, *scales, dense, (hipStream_t)stream)
+                              : prhs::launch_attention(a, dense, (hipStream_t)stream),
+                       name);
 }
 
 prhs_status prhs_sparse_decode_attn(const prhs_kv* kv, const void* q, const int32_t* set_idx,
                                     const int32_t* set_len, int32_t set_cap, float scale,
                                     float* out, float* lse, void* ws, size_t ws_bytes,
                                     void* stream) {
-  return attention_common(kv, q, set_idx, set_len, set_cap, nullptr, nullptr, nullptr, 0, nullptr,
+  return attention_common(kv, nullptr, q, set_idx, set_len, set_cap, nullptr, nullptr, nullptr, 0, nullptr,
                           0, nullptr, scale, out, lse, ws, ws_bytes, stream, false,
                           "prhs_sparse_decode_attn launch");
 }
@@ -408,14 +476,14 @@ prhs_status prhs_sparse_decode_attn_static(const prhs_kv* kv, const void* q,
     return fail(PRHS_E_UNSUPPORTED,
                 "split-K partials of %zu bytes exceed the static scratch of %zu bytes", need,
                 prhs::kStaticScratchBytes);
-  if (kv->batch == 0) return attention_common(kv, q, set_idx, set_len, set_cap, nullptr, nullptr,
+  if (kv->batch == 0) return attention_common(kv, nullptr, q, set_idx, set_len, set_cap, nullptr, nullptr,
                                               nullptr, 0, nullptr, 0, nullptr, scale, out, lse,
                                               nullptr, 0, stream, false,
                                               "prhs_sparse_decode_attn_static");
   void* ws = nullptr;
   if ((st = device_status(prhs::attn_static_scratch(&ws), "static scratch lookup")) != PRHS_OK)
     return st;
-  return attention_common(kv, q, set_idx, set_len, set_cap, nullptr, nullptr, nullptr, 0, nullptr,
+  return attention_common(kv, nullptr, q, set_idx, set_len, set_cap, nullptr, nullptr, nullptr, 0, nullptr,
                           0, nullptr, scale, out, lse, ws, prhs::kStaticScratchBytes, stream, false,
                           "prhs_sparse_decode_attn_static launch");
 }
@@ -426,17 +494,18 @@ prhs_status prhs_reuse_decode_attn(const prhs_kv* kv, const void* q, const int32
                                    void* ws, size_t ws_bytes, void* stream) {
   if (kv && kv->batch > 0 && !anchor_lens)
     return fail(PRHS_E_INVALID, "anchor_lens must be non-NULL");
-  return attention_common(kv, q, set_idx, set_len, set_cap, anchor_lens, nullptr, nullptr, 0,
+  return attention_common(kv, nullptr, q, set_idx, set_len, set_cap, anchor_lens, nullptr, nullptr, 0,
                           nullptr, 0, nullptr, scale, out, lse, ws, ws_bytes, stream, false,
                           "prhs_reuse_decode_attn launch");
 }
 
-prhs_status prhs_pool_decode_attn(const prhs_kv* kv, const void* q, const int32_t* pool_idx,
+static prhs_status pool_common(const prhs_kv* kv, const prhs::QuantScales* scales, const void* q, const int32_t* pool_idx,
                                   const int32_t* pool_len, int32_t pool_rows, int32_t set_cap,
                                   const int32_t* unit_row, const int32_t* unit_tail,
                                   const int32_t* unit_gate, int32_t units_side,
                                   const prhs_psaw* psaw, float scale, float* out, float* lse,
-                                  void* ws, size_t ws_bytes, void* stream) {
+                                  void* ws, size_t ws_bytes, void* stream,
+                               const char* name) {
   if (pool_rows < 0) return fail(PRHS_E_INVALID, "pool_rows must be >= 0");
   if (kv && kv->batch > 0 && (!unit_row || !unit_tail))
     return fail(PRHS_E_INVALID, "unit_row and unit_tail must be non-NULL");
@@ -445,9 +514,20 @@ prhs_status prhs_pool_decode_attn(const prhs_kv* kv, const void* q, const int32_
     return fail(PRHS_E_INVALID, "units_side must be PRHS_UNITS_ALL, _RETRIEVING or _SHARING");
   if (units_side != PRHS_UNITS_ALL && kv && kv->batch > 0 && !unit_gate)
     return fail(PRHS_E_INVALID, "unit_gate must be non-NULL with a units_side filter");
-  return attention_common(kv, q, pool_idx, pool_len, set_cap, nullptr, unit_row, unit_tail,
+  return attention_common(kv, scales, q, pool_idx, pool_len, set_cap, nullptr, unit_row, unit_tail,
                           pool_rows, unit_gate, units_side, psaw, scale, out, lse, ws, ws_bytes,
-                          stream, false, "prhs_pool_decode_attn launch");
+                          stream, false, name);
+}
+
+prhs_status prhs_pool_decode_attn(const prhs_kv* kv, const void* q, const int32_t* pool_idx,
+                                  const int32_t* pool_len, int32_t pool_rows, int32_t set_cap,
+                                  const int32_t* unit_row, const int32_t* unit_tail,
+                                  const int32_t* unit_gate, int32_t units_side,
+                                  const prhs_psaw* psaw, float scale, float* out, float* lse,
+                                  void* ws, size_t ws_bytes, void* stream) {
+  return pool_common(kv, nullptr, q, pool_idx, pool_len, pool_rows, set_cap, unit_row, unit_tail,
+                     unit_gate, units_side, psaw, scale, out, lse, ws, ws_bytes, stream,
+                     "prhs_pool_decode_attn launch");
 }
 
 static prhs_status gate_args(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
@@ -555,9 +635,218 @@ prhs_status prhs_prefill_attn(const prhs_kv* kv, const void* q, int32_t q_len,
 
 prhs_status prhs_dense_decode_attn(const prhs_kv* kv, const void* q, float scale, float* out,
                                    float* lse, void* ws, size_t ws_bytes, void* stream) {
-  return attention_common(kv, q, nullptr, nullptr, 0, nullptr, nullptr, nullptr, 0, nullptr, 0,
+  return attention_common(kv, nullptr, q, nullptr, nullptr, 0, nullptr, nullptr, nullptr, 0, nullptr, 0,
                           nullptr, scale, out, lse, ws, ws_bytes, stream, true,
                           "prhs_dense_decode_attn launch");
+}
+
+// ---- 8-bit cache ----
+
+prhs_status prhs_quant_store(const prhs_quant_kv* kv, const void* k_new, const void* v_new,
+                             int32_t new_cap, const int32_t* new_lens, const prhs_bounds* bounds,
+                             void* stream) {
+  int shift = 0, bshift = 0;
+  prhs_status st = check_quant_kv(kv, &shift);
+  if (st != PRHS_OK) return st;
+  if (bounds) {
+    if ((st = check_bounds(&kv->kv, bounds, &bshift)) != PRHS_OK) return st;
+    if (bshift != shift)
+      return fail(PRHS_E_INVALID, "the bounds' block_size (%d) differs from the cache's (%d)",
+                  bounds->block_size, kv->block_size);
+  }
+  if (new_cap < 0) return fail(PRHS_E_INVALID, "new_cap must be >= 0 (got %d)", new_cap);
+  if ((st = check_grid((long long)kv->kv.batch * kv->kv.num_kv_heads *
+                       (ceil_div(std::min(new_cap, kv->kv.max_seq_len), kv->block_size) + 1))) != PRHS_OK)
+    return st;
+  if (kv->kv.batch == 0 || new_cap == 0) return PRHS_OK;
+  if (!k_new || !v_new) return fail(PRHS_E_INVALID, "k_new and v_new must be non-NULL");
+  prhs::QuantStoreLaunch a;
+  a.kv = view_of(&kv->kv);
+  a.dtype = kv->kv.dtype;
+  a.block_shift = shift;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.tok.lens = new_lens;
+  a.tok.cap = new_cap;
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
+  a.k_min = bounds ? bounds->k_min : nullptr;
+  a.k_max = bounds ? bounds->k_max : nullptr;
+  return device_status(prhs::launch_quant_store(a, (hipStream_t)stream), "prhs_quant_store launch");
+}
+
+static prhs_status quant_scales(const prhs_quant_kv* kv, prhs::QuantScales* scales) {
+  prhs_status st = check_quant_kv(kv, &scales->block_shift);
+  if (st != PRHS_OK) return st;
+  scales->k = kv->k_scale;
+  scales->v = kv->v_scale;
+  return PRHS_OK;
+}
+
+prhs_status prhs_quant_sparse_decode_attn(const prhs_quant_kv* kv, const void* q,
+                                          const int32_t* set_idx, const int32_t* set_len,
+                                          int32_t set_cap, float scale, float* out, float* lse,
+                                          void* ws, size_t ws_bytes, void* stream) {
+  prhs::QuantScales sc;
+  prhs_status st = quant_scales(kv, &sc);
+  if (st != PRHS_OK) return st;
+  return attention_common(&kv->kv, &sc, q, set_idx, set_len, set_cap, nullptr, nullptr, nullptr, 0,
+                          nullptr, 0, nullptr, scale, out, lse, ws, ws_bytes, stream, false,
+                          "prhs_quant_sparse_decode_attn launch");
+}
+
+prhs_status prhs_quant_reuse_decode_attn(const prhs_quant_kv* kv, const void* q,
+                                         const int32_t* set_idx, const int32_t* set_len,
+                                         int32_t set_cap, const int32_t* anchor_lens, float scale,
+                                         float* out, float* lse, void* ws, size_t ws_bytes,
+                                         void* stream) {
+  prhs::QuantScales sc;
+  prhs_status st = quant_scales(kv, &sc);
+  if (st != PRHS_OK) return st;
+  if (kv->kv.batch > 0 && !anchor_lens)
+    return fail(PRHS_E_INVALID, "anchor_lens must be non-NULL");
+  return attention_common(&kv->kv, &sc, q, set_idx, set_len, set_cap, anchor_lens, nullptr, nullptr,
+                          0, nullptr, 0, nullptr, scale, out, lse, ws, ws_bytes, stream, false,
+                          "prhs_quant_reuse_decode_attn launch");
+}
+
+prhs_status prhs_quant_dense_decode_attn(const prhs_quant_kv* kv, const void* q, float scale,
+                                         float* out, float* lse, void* ws, size_t ws_bytes,
+                                         void* stream) {
+  prhs::QuantScales sc;
+  prhs_status st = quant_scales(kv, &sc);
+  if (st != PRHS_OK) return st;
+  return attention_common(&kv->kv, &sc, q, nullptr, nullptr, 0, nullptr, nullptr, nullptr, 0, nullptr,
+                          0, nullptr, scale, out, lse, ws, ws_bytes, stream, true,
+                          "prhs_quant_dense_decode_attn launch");
+}
+
+prhs_status prhs_quant_pool_decode_attn(const prhs_quant_kv* kv, const void* q,
+                                        const int32_t* pool_idx, const int32_t* pool_len,
+                                        int32_t pool_rows, int32_t set_cap,
+                                        const int32_t* unit_row, const int32_t* unit_tail,
+                                        const int32_t* unit_gate, int32_t units_side,
+                                        const prhs_psaw* psaw, float scale, float* out, float* lse,
+                                        void* ws, size_t ws_bytes, void* stream) {
+  prhs::QuantScales sc;
+  prhs_status st = quant_scales(kv, &sc);
+  if (st != PRHS_OK) return st;
+  return pool_common(&kv->kv, &sc, q, pool_idx, pool_len, pool_rows, set_cap, unit_row, unit_tail,
+                     unit_gate, units_side, psaw, scale, out, lse, ws, ws_bytes, stream,
+                     "prhs_quant_pool_decode_attn launch");
+}
+
+// ---- blocks ----
+
+prhs_status prhs_block_bounds(const prhs_kv* kv, const prhs_bounds* bounds, int32_t new_cap,
+                              const int32_t* new_lens, void* stream) {
+  prhs_status st = check_kv_shape(kv);
+  if (st != PRHS_OK) return st;
+  if ((st = check_kv_data(kv)) != PRHS_OK) return st;
+  int shift = 0;
+  if ((st = check_bounds(kv, bounds, &shift)) != PRHS_OK) return st;
+  if (new_cap < 0) return fail(PRHS_E_INVALID, "new_cap must be >= 0 (got %d)", new_cap);
+  if ((st = check_grid((long long)kv->batch * kv->num_kv_heads *
+                       (ceil_div(std::min(new_cap, kv->max_seq_len), bounds->block_size) + 1))) != PRHS_OK)
+    return st;
+  if (kv->batch == 0 || new_cap == 0) return PRHS_OK;
+  prhs::BlockBoundsLaunch a;
+  a.kv = view_of(kv);
+  a.dtype = kv->dtype;
+  a.block_shift = shift;
+  a.tok.lens = new_lens;
+  a.tok.cap = new_cap;
+  a.k_min = bounds->k_min;
+  a.k_max = bounds->k_max;
+  return device_status(prhs::launch_block_bounds(a, (hipStream_t)stream), "prhs_block_bounds launch");
+}
+
+// Candidates and budget both grow with the length, so their minimum peaks at
+// the longest sequence.
+int32_t prhs_max_blocks(const prhs_params* p, int32_t block_size, int32_t max_seq_len) {
+  if (check_params(p) != PRHS_OK) return -1;
+  if (max_seq_len < 0 ||
+      (block_size != 16 && block_size != 32 && block_size != 64 && block_size != 128)) {
+    fail(PRHS_E_INVALID, "max_seq_len must be >= 0 and block_size 16, 32, 64 or 128");
+    return -1;
+  }
+  const long long mid = middle_at(p, max_seq_len), first = p->sink / block_size;
+  if (mid <= 0) return 0;
+  const long long cand = (p->sink + mid - 1) / block_size + 1 - first;
+  return (int32_t)std::min(ceil_div(budget_at(p, max_seq_len), block_size), cand);
+}
+
+int32_t prhs_block_set_capacity(const prhs_params* p, int32_t block_size, int32_t max_seq_len) {
+  const int32_t blocks = prhs_max_blocks(p, block_size, max_seq_len);
+  if (blocks < 0) return -1;
+  const long long cap = (long long)p->sink + (long long)blocks * block_size + p->window +
+                        (p->refresh_every - 1);
+  return (int32_t)std::min(cap, (long long)max_seq_len);
+}
+
+prhs_status prhs_block_workspace_size(const prhs_kv* kv, const prhs_bounds* bounds, size_t* bytes) {
+  if (!bytes) return fail(PRHS_E_INVALID, "bytes is NULL");
+  *bytes = 0;
+  prhs_status st = check_kv_shape(kv);
+  if (st != PRHS_OK) return st;
+  if (!bounds) return fail(PRHS_E_INVALID, "bounds is NULL");
+  int shift = 0;
+  if ((st = check_blocks(kv, bounds->block_size, &shift)) != PRHS_OK) return st;
+  *bytes = prhs::block_select_workspace_bytes(kv->batch * kv->num_kv_heads, kv->max_seq_len, shift);
+  return PRHS_OK;
+}
+
+prhs_status prhs_block_select(const prhs_kv* kv, const void* q, const prhs_params* params,
+                              const prhs_bounds* bounds, int32_t* blk_idx, int32_t* blk_len,
+                              int32_t blk_cap, int32_t* set_idx, int32_t* set_len,
+                              int32_t set_cap, void* ws, size_t ws_bytes, void* stream) {
+  prhs_status st = check_kv_shape(kv);
+  if (st != PRHS_OK) return st;
+  if ((st = check_params(params)) != PRHS_OK) return st;
+  int shift = 0;
+  if ((st = check_bounds(kv, bounds, &shift)) != PRHS_OK) return st;
+  if (kv->batch > 0) {
+    if (!kv->seq_lens) return fail(PRHS_E_INVALID, "seq_lens is NULL");
+    if (kv->layout == PRHS_KV_PAGED && !kv->block_table)
+      return fail(PRHS_E_INVALID, "block_table is NULL for a paged cache");
+    if (!q || !blk_idx || !blk_len || !set_idx || !set_len)
+      return fail(PRHS_E_INVALID, "q, blk_idx, blk_len, set_idx and set_len must be non-NULL");
+  }
+  const int32_t blocks = prhs_max_blocks(params, bounds->block_size, kv->max_seq_len);
+  if (blk_cap < blocks || blk_cap < 0)
+    return fail(PRHS_E_CAPACITY, "blk_cap (%d) < most chosen blocks (%d)", blk_cap, blocks);
+  const long long need = std::min((long long)kv->max_seq_len,
+                                  (long long)params->sink + (long long)blocks * bounds->block_size +
+                                      params->window);
+  if (set_cap < need || set_cap < 0)
+    return fail(PRHS_E_CAPACITY, "set_cap (%d) < the set's bound (%lld)", set_cap, need);
+  const long long units = (long long)kv->batch * kv->num_kv_heads;
+  if ((st = check_grid(units * (ceil_div(kv->max_seq_len, bounds->block_size) / 16 + 1))) != PRHS_OK)
+    return st;
+  const size_t wsz = prhs::block_select_workspace_bytes((int)units, kv->max_seq_len, shift);
+  if (wsz > 0 && (!ws || ws_bytes < wsz))
+    return fail(PRHS_E_WORKSPACE, "workspace of %zu bytes needed (got %zu)", wsz, ws_bytes);
+  if (kv->batch == 0) return PRHS_OK;
+  prhs::BlockSelectLaunch a;
+  a.kv = view_of(kv);
+  a.q = q;
+  a.dtype = kv->dtype;
+  a.block_shift = shift;
+  a.k_min = bounds->k_min;
+  a.k_max = bounds->k_max;
+  a.k = params->k;
+  a.k_num = params->k_num;
+  a.k_den = params->k_den;
+  a.sink = params->sink;
+  a.window = params->window;
+  a.blk_idx = blk_idx;
+  a.blk_len = blk_len;
+  a.blk_cap = blk_cap;
+  a.set_idx = set_idx;
+  a.set_len = set_len;
+  a.set_cap = set_cap;
+  a.ws = ws;
+  return device_status(prhs::launch_block_select(a, (hipStream_t)stream), "prhs_block_select launch");
 }
 
 }  // extern "C"

@@ -318,6 +318,76 @@ struct PrefillLaunch {
 };
 hipError_t launch_prefill(const PrefillLaunch& a, hipStream_t stream);
 
+// ---- 8-bit cache and block selection ----
+
+// Where a store or a bounds update finds its tokens: the last new_tokens()
+// positions of every sequence.
+struct NewTokens {
+  const int32_t* lens;  // [B] or null: cap of each
+  int cap;
+};
+__device__ __forceinline__ int new_tokens(const NewTokens& t, int b, int n) {
+  int c = t.cap;
+  if (t.lens) c = min(max(t.lens[b], 0), c);
+  return min(c, n);
+}
+
+struct QuantStoreLaunch {
+  KvView kv;            // k and v: e4m3 bytes, written
+  int dtype;            // of the new keys and values, and of the bounds
+  int block_shift;      // log2 of the tokens per scale
+  const void* k_new;    // [B][Hkv][tok.cap][d]
+  const void* v_new;
+  NewTokens tok;
+  float* k_scale;
+  float* v_scale;
+  void* k_min;          // or null
+  void* k_max;
+};
+hipError_t launch_quant_store(const QuantStoreLaunch& a, hipStream_t stream);
+
+struct BlockBoundsLaunch {
+  KvView kv;
+  int dtype;
+  int block_shift;
+  NewTokens tok;
+  void* k_min;
+  void* k_max;
+};
+hipError_t launch_block_bounds(const BlockBoundsLaunch& a, hipStream_t stream);
+
+struct BlockSelectLaunch {
+  KvView kv;
+  const void* q;
+  int dtype;
+  int block_shift;
+  const void* k_min;
+  const void* k_max;
+  int k, k_num, k_den, sink, window;
+  int32_t* blk_idx;
+  int32_t* blk_len;
+  int blk_cap;
+  int32_t* set_idx;
+  int32_t* set_len;
+  int set_cap;
+  void* ws;
+};
+size_t block_select_workspace_bytes(int units, int max_seq_len, int block_shift);
+hipError_t launch_block_select(const BlockSelectLaunch& a, hipStream_t stream);
+
+// Attention over the 8-bit cache: an AttnLaunch whose kv.k and kv.v are e4m3
+// bytes and whose dtype is that of q.
+struct QuantScales {
+  const float* k;
+  const float* v;
+  int block_shift;
+};
+long long quant_attn_groups(bool dense, int batch, int hkv, int rows_cap);   // workgroups
+size_t quant_attn_call_bytes(bool dense, int batch, int hq, int hkv, int d, int rows_cap);
+size_t quant_attn_workspace_bytes(bool dense, int batch, int hq, int hkv, int d, int rows_cap);
+hipError_t launch_quant_attention(const AttnLaunch& a, const QuantScales& scales, bool dense,
+                                  hipStream_t stream);
+
 // Compute units of the current device (cached per device; 0 if unknown).
 int device_cus();
 

@@ -1,0 +1,651 @@
+"""The 8-bit KV cache on the GPU against its fp64 oracle: the store, attention
+over the cache, key bounds and the selection of blocks.
+
+Attention tolerance.  With u = 2^-24, a logit x = scale sum_d q_d k_d is off by
+at most dx = (d + 8) u scale sum_d |q_d k_d| + 4 u |x| (fp32 products and sums,
+scale factors, the exponent's argument), a weight by dx and 2^-21 relative (the
+exponential, its fp16 pair), and fp32 sums of at most n / 32 + 64 terms by as
+many u.  y is off by at most twice the weights' relative error times max |v|,
+lse by the weights' relative error and 4 u |lse|."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle as O
+from oracle import quant_oracle as Q
+from paper_2602_08329_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+E4 = torch.float8_e4m3fn
+I32 = torch.int32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+class Cache:
+    """A seeded 8-bit cache on the host (NumPy) and its copy on the GPU.  Rows at
+    and behind a sequence's length, and unused pages, hold NaN bytes and NaN
+    scales of blocks no token lies in."""
+
+    def __init__(self, lens, hq, hkv, d, bs=16, paged=False, dtype="bf16", seed=0, spread=3.0,
+                 fill=True, cap=None):
+        rng = np.random.default_rng(seed)
+        self.lens, self.hq, self.hkv, self.d, self.bs, self.paged = lens, hq, hkv, d, bs, paged
+        self.dtype = torch.float32 if dtype == "f32" else torch.bfloat16
+        n_cap = max(max(lens), 1) if cap is None else cap
+        self.nb = -(-n_cap // bs)
+        Bn = len(lens)
+        self.pages = Bn * self.nb + 3 if paged else 0
+        blocks = self.pages * hkv if paged else Bn * hkv * self.nb
+        self.table = rng.permutation(self.pages)[: Bn * self.nb].reshape(Bn, self.nb) if paged else None
+        self.raw = {x: np.full((blocks, bs, d), 127, np.uint8) for x in "kv"}
+        self.scale = {x: np.full(blocks, np.nan, np.float32) for x in "kv"}
+        if fill:
+            for b, n in enumerate(lens):
+                for g in range(hkv):
+                    for j in range(-(-n // bs)):
+                        i, r = self.block(b, g, j), min(bs, n - j * bs)
+                        for x in "kv":
+                            v = rng.integers(0, 127, (r, d)) * 1 + 128 * rng.integers(0, 2, (r, d))
+                            self.raw[x][i, :r] = v
+                            # K: unit logits whatever the scale's spread
+                            s = 2.0 ** rng.uniform(-spread, spread)
+                            self.scale[x][i] = s / (200 if x == "k" else 100)
+        shape = (self.pages, hkv, bs, d) if paged else (Bn, hkv, self.nb * bs, d)
+        sshape = (self.pages, hkv) if paged else (Bn, hkv, self.nb)
+        dev = {x: torch.tensor(self.raw[x]).to(DEV).view(E4).view(shape) for x in "kv"}
+        dsc = {x: torch.tensor(self.scale[x]).to(DEV).view(sshape) for x in "kv"}
+        self.dev, self.dsc = dev, dsc
+        self.seq = torch.tensor(lens, dtype=I32, device=DEV)
+        self.dtable = torch.tensor(self.table, dtype=I32, device=DEV) if paged else None
+        self.kv = B.QuantKV(dev["k"], dev["v"], dsc["k"], dsc["v"], self.seq, n_cap, hq, self.dtable,
+                            dtype=self.dtype)
+        q = rng.standard_normal((Bn, hq, d))
+        self.q = torch.tensor(q, dtype=torch.float32).to(self.dtype).to(DEV)
+        self.scale_q = 1 / math.sqrt(d)
+
+    def block(self, b, g, j):
+        if self.paged:
+            return int(self.table[b, j]) * self.hkv + g
+        return (b * self.hkv + g) * self.nb + j
+
+    def values(self, x, b, g, n):
+        """Rows [0, n) of a unit in fp64."""
+        rows = [Q.TABLE[self.raw[x][self.block(b, g, j)]] * float(self.scale[x][self.block(b, g, j)])
+                for j in range(-(-n // self.bs))]
+        return np.concatenate(rows)[:n] if rows else np.zeros((0, self.d))
+
+    def outputs(self):
+        Bn = len(self.lens)
+        return (torch.full((Bn, self.hq, self.d), 7.0, device=DEV),
+                torch.full((Bn, self.hq), 7.0, device=DEV))
+
+    def workspace(self, dense, cap=0):
+        """Exactly the bytes asked for, followed by bytes that must stay."""
+        op = B.PRHS_OP_QUANT_DENSE_ATTN if dense else B.PRHS_OP_QUANT_SPARSE_ATTN
+        n = B.prhs_workspace_size(op, self.kv, None, cap)
+        self.ws_all = torch.full((n + 256,), 255, dtype=torch.uint8, device=DEV)
+        return self.ws_all[:n]
+
+    def check(self, y, lse, attended, some=None):
+        """attended(b, g): positions, of the units `some` (all by default)."""
+        assert (self.ws_all[-256:] == 255).all()
+        y, lse = y.double().cpu().numpy(), lse.double().cpu().numpy()
+        q = self.q.double().cpu().numpy()
+        G, u = self.hq // self.hkv, 2.0 ** -24
+        for b in range(len(self.lens)):
+            for g in range(self.hkv):
+                if some is not None and (b, g) not in some:
+                    continue
+                S = np.asarray(attended(b, g), dtype=np.int64)
+                K, V = (self.values(x, b, g, self.lens[b])[S] for x in "kv")
+                for h in range(g * G, (g + 1) * G):
+                    if not len(S):
+                        assert (y[b, h] == 0).all() and lse[b, h] == -math.inf
+                        continue
+                    yr, lr = O.dense_attention(q[b, h], K, V, self.scale_q)
+                    x = np.abs(K @ q[b, h]) * self.scale_q
+                    dx = ((self.d + 8) * u * self.scale_q * (np.abs(K) @ np.abs(q[b, h]))).max() + 4 * u * x.max()
+                    rel = dx + 2.0 ** -21 + (len(S) / 32 + 64) * u
+                    top = np.abs(V).max()
+                    assert np.abs(y[b, h] - yr).max() <= 2 * rel * top, (b, h, np.abs(y[b, h] - yr).max(), 2 * rel * top)
+                    assert abs(lse[b, h] - lr) <= rel + 4 * u * abs(lr), (b, h, lse[b, h], lr)
+
+
+def dense(c):
+    y, lse = c.outputs()
+    B.prhs_quant_dense_decode_attn(c.kv, c.q, c.scale_q, y, lse, c.workspace(True))
+    return y, lse
+
+
+def pack(sets, batch, hkv, cap, fill=-7):
+    idx = torch.full((batch, hkv, cap), fill, dtype=I32)
+    ln = torch.zeros(batch, hkv, dtype=I32)
+    for (b, g), S in sets.items():
+        idx[b, g, : len(S)] = torch.tensor(list(S), dtype=I32)
+        ln[b, g] = len(S)
+    return idx.to(DEV), ln.to(DEV)
+
+
+HEADS = [(1, 1), (2, 2), (6, 2), (5, 1), (8, 1), (18, 2), (16, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,bs,paged", [(128, 16, True), (64, 16, False), (128, 64, False), (64, 128, True), (128, 32, True)])
+def test_dense_lengths_around_tiles_and_blocks(d, bs, paged, dtype):
+    lens = (0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 300)
+    hq, hkv = HEADS[(d + bs) % len(HEADS)]
+    c = Cache(lens, hq, hkv, d, bs, paged, dtype, seed=d + bs)
+    c.check(*dense(c), lambda b, g: range(lens[b]))
+
+
+@pytest.mark.parametrize("hq,hkv", HEADS)
+def test_dense_head_groups(hq, hkv):
+    lens = (200, 77)
+    for d, dtype in ((128, "bf16"), (64, "f32")):
+        c = Cache(lens, hq, hkv, d, seed=hq)
+        c.check(*dense(c), lambda b, g: range(lens[b]))
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d,paged,dtype", [
+    ((9001,), 4, 1, 128, True, "bf16"),            # one unit in many splits
+    ((5000, 4999, 33, 2500), 8, 2, 64, False, "bf16"),
+    ((2048, 2049), 16, 1, 128, False, "f32"),
+    (tuple(700 - 3 * i for i in range(40)), 8, 8, 64, True, "bf16"),    # 320 units
+])
+def test_dense_splits(lens, hq, hkv, d, paged, dtype):
+    c = Cache(lens, hq, hkv, d, 16, paged, dtype, seed=lens[0])
+    some = {(b, g) for b in (0, 1, len(lens) // 2, len(lens) - 1) for g in (0, hkv - 1) if b < len(lens)}
+    c.check(*dense(c), lambda b, g: range(lens[b]), some)
+
+
+@pytest.mark.parametrize("spread", [0.0, 10.0])
+def test_scales_far_apart(spread):
+    # block scales of V over a factor of 2^20: weights of the smaller blocks keep
+    # 2^-32 of the largest one's
+    c = Cache((500, 40), 4, 2, 128, 16, True, "bf16", seed=3, spread=spread)
+    for x in "k":   # logits stay moderate
+        c.scale[x][:] = np.where(np.isnan(c.scale[x]), np.nan, np.float32(1 / 300))
+        c.dsc[x].copy_(torch.tensor(c.scale[x]).view(c.dsc[x].shape))
+    c.check(*dense(c), lambda b, g: range(c.lens[b]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,bs,paged,cap", [(128, 16, True, 40), (64, 32, False, 600), (128, 64, True, 1500), (128, 128, False, 3000)])
+def test_sparse_sets(d, bs, paged, cap, dtype):
+    # entries outside the sequence and empty sets; a set longer than its capacity
+    # says; entries in any order, one of them twice counts twice
+    rng = np.random.default_rng(cap)
+    lens = (cap * 2, 1, 5, cap // 2 + 1)
+    hq, hkv = 8, 2
+    c = Cache(lens, hq, hkv, d, bs, paged, dtype, seed=cap + d)
+    sets, want = {}, {}
+    for b, n in enumerate(lens):
+        for g in range(hkv):
+            S = rng.permutation(n)[: int(rng.integers(0, min(n, cap) + 1))]
+            if (b, g) == (0, 0):
+                S = rng.permutation(n)[:cap]
+            if (b, g) == (0, 1):
+                S = np.concatenate([S[: cap - 4], [-1, n, 1 << 21, -(1 << 30)]])
+            if (b, g) == (2, 0):
+                S = np.array([], np.int64)
+            if (b, g) == (2, 1):
+                S = np.array([1 << 21, -5])
+            sets[b, g] = S
+            want[b, g] = [p for p in S if 0 <= p < n]
+    idx, ln = pack(sets, len(lens), hkv, cap)
+    ln[0, 0] = cap + 1000
+    y, lse = c.outputs()
+    B.prhs_quant_sparse_decode_attn(c.kv, c.q, idx, ln, c.scale_q, y, lse, c.workspace(False, cap))
+    c.check(y, lse, lambda b, g: want[b, g])
+
+
+@pytest.mark.parametrize("d,paged,cap", [(128, True, 100), (64, False, 900)])
+def test_reuse_tail(d, paged, cap):
+    rng = np.random.default_rng(cap)
+    lens, anchors = (cap + 50, 20, 7, cap), (cap + 43, 20, 0, cap + 5)
+    c = Cache(lens, 6, 2, d, 16, paged, "bf16", seed=cap)
+    sets, want = {}, {}
+    for b, n in enumerate(lens):
+        n0 = min(anchors[b], n)
+        for g in range(2):
+            S = np.sort(rng.permutation(n)[: cap // 2])
+            sets[b, g], want[b, g] = S, [p for p in S if p < n0] + list(range(n0, n))
+    idx, ln = pack(sets, len(lens), 2, cap)
+    a = torch.tensor(anchors, dtype=I32, device=DEV)
+    y, lse = c.outputs()
+    B.prhs_quant_reuse_decode_attn(c.kv, c.q, idx, ln, a, c.scale_q, y, lse, c.workspace(False, cap))
+    c.check(y, lse, lambda b, g: want[b, g])
+
+
+def test_pool_rows_sides_and_window():
+    rng = np.random.default_rng(4)
+    lens, hkv, cap = (400, 90), 2, 120
+    c = Cache(lens, 4, hkv, 128, 16, True, "bf16", seed=6)
+    pool = [np.sort(rng.permutation(90)[:50]) for _ in range(5)]
+    idx = torch.zeros(5, cap, dtype=I32)
+    for r, S in enumerate(pool):
+        idx[r, :50] = torch.tensor(S)
+    plen = torch.full((5,), 50, dtype=I32, device=DEV)
+    rows, tails, gate = [3, 9, 0, 4], [395, 390, 90, 60], [-1, 2, 1, -1]
+    rows_d, tails_d, gate_d = (torch.tensor(x, dtype=I32, device=DEV) for x in (rows, tails, gate))
+    ps = B.psaw(3, 4, 1, 0.5, 1.0, 8)
+
+    def want(b, g, window):
+        u, n = b * hkv + g, lens[b]
+        if rows[u] >= 5:
+            return []
+        S = [p for p in pool[rows[u]] if p < tails[u]] + list(range(min(tails[u], n), n))
+        first = B.prhs_psaw_first_visible(ps, n)
+        return [p for p in S if not window or p < 8 or p >= first]
+
+    for window in (False, True):
+        y, lse = c.outputs()
+        for side in (B.PRHS_UNITS_RETRIEVING, B.PRHS_UNITS_SHARING):
+            B.prhs_quant_pool_decode_attn(c.kv, c.q, idx.to(DEV), plen, rows_d, tails_d, c.scale_q, y, lse,
+                                          c.workspace(False, cap), psaw=ps if window else None,
+                                          unit_gate=gate_d, units_side=side)
+            if side == B.PRHS_UNITS_RETRIEVING:   # the others are left as they are
+                assert (y[0, 2:] == 7).all() and (y[1, :2] == 7).all() and not (y[0, :2] == 7).any()
+        c.check(y, lse, lambda b, g: want(b, g, window))
+
+
+def test_pages_outside_the_pool_and_lengths_beyond_the_bound():
+    lens = (100, 64)
+    c = Cache(lens, 4, 2, 128, 16, True, "bf16", seed=8)
+    t = c.dtable.clone()
+    t[0, 2], t[0, 6], t[1, 0] = -1, c.pages, 1 << 30
+    c.dtable.copy_(t)
+    y, lse = c.outputs()
+    B.prhs_quant_dense_decode_attn(c.kv, c.q, c.scale_q, y, lse, c.workspace(True))
+    left = ([p for p in range(100) if p // 16 not in (2, 6)], list(range(16, 64)))
+    c.check(y, lse, lambda b, g: left[b])
+    # a length above max_seq_len counts as max_seq_len, a negative one as none
+    c.seq.copy_(torch.tensor([1000, -3], dtype=I32))
+    y, lse = c.outputs()
+    B.prhs_quant_dense_decode_attn(c.kv, c.q, c.scale_q, y, lse, c.workspace(True))
+    c.lens = (100, 0)
+    c.check(y, lse, lambda b, g: left[b] if b == 0 else [])
+
+
+def test_no_lse_and_another_stream():
+    c = Cache((500, 60), 8, 2, 128, 16, True, "bf16", seed=9)
+    y0, _ = dense(c)
+    s = torch.cuda.Stream()
+    y1, _ = c.outputs()
+    ws = c.workspace(True)
+    s.wait_stream(torch.cuda.current_stream())
+    B.prhs_quant_dense_decode_attn(c.kv, c.q, c.scale_q, y1, None, ws, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(y0, y1)
+
+
+# ---- the store --------------------------------------------------------------------
+
+class Store:
+    """A cache that tokens are stored into, on both sides."""
+
+    def __init__(self, batch, hkv, d, bs, paged, dtype, cap, seed, bounds=True):
+        self.c = Cache((0,) * batch, hkv, hkv, d, bs, paged, dtype, seed=seed, fill=False, cap=cap)
+        self.rng = np.random.default_rng(seed + 1)
+        self.n = [0] * batch
+        c = self.c
+        blocks = len(c.scale["k"])
+        self.lo, self.hi = np.full((blocks, d), 9.0), np.full((blocks, d), -9.0)
+        sh = (c.pages, hkv, d) if paged else (batch, hkv, c.nb, d)
+        self.dlo, self.dhi = (torch.tensor(x, dtype=c.dtype, device=DEV).view(sh) for x in (self.lo, self.hi))
+        self.bounds = B.BlockBounds(c.kv, self.dlo, self.dhi) if bounds else None
+
+    def tokens(self, T, wide=4.0):
+        c = self.c
+        x = self.rng.standard_normal((2, len(self.n), c.hkv, T, c.d)) * 2.0 ** self.rng.uniform(-wide, wide, (2, len(self.n), c.hkv, T, 1))
+        return [torch.tensor(y, dtype=torch.float32).to(c.dtype) for y in x]
+
+    def store(self, k, v, new=None, dropped=()):
+        """new: tokens of each sequence (all of k's by default)."""
+        c, T = self.c, k.shape[2]
+        new = [T] * len(self.n) if new is None else new
+        for b, t in enumerate(new):
+            first, self.n[b] = self.n[b], self.n[b] + t
+            for g in range(c.hkv):
+                for j in range(first // c.bs, -(-self.n[b] // c.bs)):
+                    a, z = max(first, j * c.bs), min(self.n[b], (j + 1) * c.bs)
+                    if z <= a or (b, j) in dropped:
+                        continue
+                    i, r0 = c.block(b, g, j), a - j * c.bs
+                    for x, src in (("k", k), ("v", v)):
+                        xs = src[b, g, a - first: z - first].double().numpy()
+                        c.raw[x][i, : z - j * c.bs], c.scale[x][i] = Q.store_block(c.raw[x][i, :r0], c.scale[x][i], xs)
+                        if x == "k" and self.bounds is not None:
+                            lo, hi = Q.block_bounds(xs)
+                            old = r0 > 0
+                            self.lo[i] = np.minimum(lo, self.lo[i]) if old else lo
+                            self.hi[i] = np.maximum(hi, self.hi[i]) if old else hi
+        c.seq.copy_(torch.tensor(self.n, dtype=I32))
+        nl = torch.tensor(new, dtype=I32, device=DEV)
+        B.prhs_quant_store(c.kv, k.to(DEV), v.to(DEV), nl, self.bounds)
+
+    def check(self):
+        c = self.c
+        for x in "kv":
+            got = c.dev[x].view(torch.uint8).cpu().numpy().reshape(c.raw[x].shape)
+            nan = (got & 127) == 127
+            want_nan = (c.raw[x] & 127) == 127
+            assert np.array_equal(nan, want_nan) and np.array_equal(got[~nan], c.raw[x][~nan])
+            assert np.array_equal(c.dsc[x].cpu().numpy().ravel(), c.scale[x], equal_nan=True)
+        assert np.array_equal(self.dlo.double().cpu().numpy().reshape(self.lo.shape), self.lo)
+        assert np.array_equal(self.dhi.double().cpu().numpy().reshape(self.hi.shape), self.hi)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,bs,paged", [(128, 16, True), (64, 16, False), (64, 32, True), (128, 64, False), (128, 128, True), (64, 128, False)])
+def test_store_prompts_chunks_and_single_tokens(d, bs, paged, dtype):
+    s = Store(3, 2, d, bs, paged, dtype, 3 * bs + 40, seed=d + bs)
+    s.store(*s.tokens(bs + 5), new=[bs + 5, 0, bs])       # ragged prompts, one empty
+    s.check()
+    for _ in range(4):                                    # single tokens
+        s.store(*s.tokens(1))
+    s.check()
+    s.store(*s.tokens(bs + 20), new=[7, bs + 20, bs])     # chunks over block edges
+    s.check()
+    s.store(*s.tokens(9), new=[0, 9, 1])
+    s.check()
+
+
+def test_store_token_by_token_over_two_blocks():
+    s = Store(2, 3, 128, 16, True, "bf16", 40, seed=5)
+    for i in range(33):
+        s.store(*s.tokens(1, wide=8.0))
+    s.check()
+
+
+def test_store_without_bounds_or_new_lens():
+    s = Store(2, 1, 64, 16, False, "f32", 64, seed=6, bounds=False)
+    k, v = s.tokens(20)
+    s.store(k, v)
+    s.check()
+    # new_lens NULL: every token; more tokens than the sequence holds: its last ones
+    c = s.c
+    c.seq.copy_(torch.tensor([20, 12], dtype=I32))
+    before = c.dev["k"].view(torch.uint8).clone()
+    B.prhs_quant_store(c.kv, k.to(DEV), v.to(DEV))
+    after = c.dev["k"].view(torch.uint8)
+    assert torch.equal(after[0], before[0])
+    want, sc = Q.store_block(np.zeros((0, 64), np.uint8), 1.0, k[1, 0, :12].double().numpy())
+    assert np.array_equal(after[1, 0, :12].cpu().numpy(), want) and float(c.dsc["k"][1, 0, 0]) == sc
+    assert torch.equal(after[1, 0, 12:], before[1, 0, 12:])
+
+
+def test_store_extreme_values():
+    d, bs = 64, 16
+    s = Store(1, 1, d, bs, False, "f32", 7 * bs, seed=7)
+    k, v = s.tokens(7 * bs)
+    k[0, 0, :16] = 0.0                                         # the smallest scale
+    k[0, 0, 16:32] *= 1e-38                                    # denormal numbers
+    k[0, 0, 32, 0], k[0, 0, 33, 1] = 3.4e38, -3.4e38           # the largest
+    k[0, 0, 48, 0], k[0, 0, 49, 1], k[0, 0, 50, 2] = math.nan, math.inf, -math.inf
+    k[0, 0, 64:80] = math.nan                                  # nothing finite
+    k[0, 0, 80:96, 0], k[0, 0, 80:96, 1] = 448.0, 480.0        # at the scale's edge
+    v[0, 0, :16] = torch.tensor([-0.0])
+    # bounds: NaN is left out, and a dimension of nothing but NaN has none
+    s.store(k, v)
+    s.check()
+    s2 = Store(1, 1, d, bs, False, "bf16", bs, seed=8)         # a zero block, then small tokens
+    z = torch.zeros(1, 1, 3, d, dtype=torch.bfloat16)
+    s2.store(z, z)
+    s2.store(*s2.tokens(2, wide=20.0))
+    s2.check()
+
+
+def test_store_drops_tokens_on_pages_outside_the_pool():
+    s = Store(2, 2, 128, 16, True, "bf16", 64, seed=9)
+    s.c.dtable[0, 1], s.c.dtable[1, 0] = -1, s.c.pages
+    s.store(*s.tokens(50), dropped={(0, 1), (1, 0)})
+    s.check()
+
+
+def test_store_is_idempotent():
+    s = Store(2, 2, 128, 16, True, "bf16", 64, seed=10)
+    s.store(*s.tokens(21))
+    k, v = s.tokens(5, wide=6.0)
+    s.store(k, v)
+    s.check()
+    B.prhs_quant_store(s.c.kv, k.to(DEV), v.to(DEV), None, s.bounds)
+    s.check()
+
+
+# ---- bounds and selection ----------------------------------------------------------
+
+def plain_cache(lens, hkv, d, bs, paged, dtype, seed, cap=None):
+    """A bf16 or fp32 cache on the grid j/16, NaN behind each sequence."""
+    rng = np.random.default_rng(seed)
+    n_cap = max(lens) if cap is None else cap
+    nb, Bn = -(-n_cap // bs), len(lens)
+    x = np.clip(np.round(rng.standard_normal((Bn, hkv, nb * bs, d)) * 16), -255, 255) / 16
+    for b, n in enumerate(lens):
+        x[b, :, n:] = np.nan
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    seq = torch.tensor(lens, dtype=I32, device=DEV)
+    if not paged:
+        K = torch.tensor(x, dtype=dt, device=DEV)
+        return x, None, seq, K
+    pages = Bn * nb + 2
+    table = rng.permutation(pages)[: Bn * nb].reshape(Bn, nb)
+    phys = np.full((pages, hkv, bs, d), np.nan)
+    phys[table.ravel()] = x.reshape(Bn, hkv, nb, bs, d).transpose(0, 2, 1, 3, 4).reshape(-1, hkv, bs, d)
+    return x, table, seq, torch.tensor(phys, dtype=dt, device=DEV)
+
+
+def bounds_of(x, lens, bs, b, g, j):
+    return Q.block_bounds(x[b, g, j * bs: min(lens[b], (j + 1) * bs)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,bs,paged", [(128, 16, True), (64, 64, False), (128, 128, False), (64, 32, True)])
+def test_block_bounds(d, bs, paged, dtype):
+    lens, hkv = (3 * bs + 5, 1, 2 * bs, 0), 2
+    x, table, seq, K = plain_cache(lens, hkv, d, bs, paged, dtype, seed=bs + d)
+    dtab = torch.tensor(table, dtype=I32, device=DEV) if paged else None
+    kv = B.KV(K, K, seq, max(lens), hkv, dtab)
+    nb = -(-max(lens) // bs)
+    shape = (K.shape[0], hkv, d) if paged else (len(lens), hkv, nb, d)
+    for new, cap in (([bs + 7, 1, 1, 0], bs + 9), (None, 1), (None, max(lens) + 50), ([0, 0, 0, 0], 4)):
+        lo, hi = (torch.full(shape, v, dtype=K.dtype, device=DEV) for v in (5.0, -5.0))
+        nl = None if new is None else torch.tensor(new, dtype=I32, device=DEV)
+        B.prhs_block_bounds(kv, B.BlockBounds(kv, lo, hi), cap, nl)
+        for b, n in enumerate(lens):
+            c = min(n, cap if new is None else min(new[b], cap))
+            for g in range(hkv):
+                for j in range(nb):
+                    at = (int(table[b, j]), g) if paged else (b, g, j)
+                    got = lo[at].double().cpu().numpy(), hi[at].double().cpu().numpy()
+                    hit = c > 0 and (n - c) // bs <= j and j * bs < n
+                    want = bounds_of(x, lens, bs, b, g, j) if hit else (np.full(d, 5.0), np.full(d, -5.0))
+                    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1]), (b, g, j, hit)
+
+
+def run_select(kv, bounds, q, p, bs, max_len, hkv, batch, spare=0):
+    kc = max(1, B.prhs_max_blocks(p, bs, max_len)) + spare
+    sc = max(1, B.prhs_block_set_capacity(p, bs, max_len)) + spare
+    blk, st = (torch.full((batch, hkv, x), -9, dtype=I32, device=DEV) for x in (kc, sc))
+    bl, sl = (torch.full((batch, hkv), -9, dtype=I32, device=DEV) for _ in range(2))
+    n = B.prhs_block_workspace_size(kv, bounds)
+    ws = torch.full((n + 256,), 255, dtype=torch.uint8, device=DEV)
+    B.prhs_block_select(kv, q, p, bounds, blk, bl, st, sl, ws[:n])
+    assert (ws[n:] == 255).all()
+    return blk, bl, st, sl
+
+
+def check_select(got, sigma, lens, hkv, kb, sink, window, bs):
+    blk, bl, st, sl = (t.cpu().numpy() for t in got)
+    for b, n in enumerate(lens):
+        for g in range(hkv):
+            cand = Q.candidate_blocks(n, sink, window, bs)
+            want = Q.choose_blocks(sigma(b, g), cand, kb(n), bs)
+            S = Q.block_set(want, n, sink, window, bs)
+            assert bl[b, g] == len(want) and blk[b, g, : len(want)].tolist() == want, (b, g, n)
+            assert sl[b, g] == len(S) and st[b, g, : len(S)].tolist() == S, (b, g, n)
+            assert (blk[b, g, len(want):] == -9).all() and (st[b, g, len(S):] == -9).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d,bs,paged,n,k,sink,window", [
+    (4, 2, 128, 16, True, 700, 96, 4, 32),
+    (16, 1, 64, 16, False, 3000, 1000, 0, 0),
+    (3, 3, 64, 32, True, 900, 65, 40, 100),        # sink and window end inside blocks
+    (5, 1, 128, 64, False, 2000, 1, 16, 64),
+    (18, 2, 128, 128, True, 1500, 600, 130, 7),
+    (8, 8, 64, 16, False, 400, 5000, 4, 16),       # the budget exceeds the candidates
+    (2, 1, 64, 16, True, 300, 0, 4, 16),           # no budget: sink and window
+    (2, 1, 64, 16, True, 17000, 512, 4, 64),       # more than a thousand blocks
+])
+def test_block_select(hq, hkv, d, bs, paged, n, k, sink, window, dtype):
+    lens = (n, 0, 1, sink + window, sink + window + 1, n - 1, min(n, sink + bs), 2 * bs)
+    lens = tuple(min(x, n) for x in lens)
+    x, table, seq, K = plain_cache(lens, hkv, d, bs, paged, dtype, seed=n + k, cap=n)
+    dtab = torch.tensor(table, dtype=I32, device=DEV) if paged else None
+    kv = B.KV(K, K, seq, n, hq, dtab)
+    nb, batch = -(-n // bs), len(lens)
+    shape = (K.shape[0], hkv, d) if paged else (batch, hkv, nb, d)
+    lo, hi = (torch.full(shape, math.nan, dtype=K.dtype, device=DEV) for _ in range(2))
+    bounds = B.BlockBounds(kv, lo, hi)
+    B.prhs_block_bounds(kv, bounds, n)
+    rng = np.random.default_rng(n)
+    q = np.clip(np.round(rng.standard_normal((batch, hq, d)) * 16), -255, 255) / 16
+    qd = torch.tensor(q, dtype=K.dtype, device=DEV)
+    G = hq // hkv
+
+    def sigma(b, g):
+        m = -(-lens[b] // bs)
+        if not m:
+            return []
+        bb = [bounds_of(x, lens, bs, b, g, j) for j in range(m)]
+        return Q.block_scores(q[b, g * G:(g + 1) * G], np.array([a for a, _ in bb]), np.array([z for _, z in bb]))
+
+    for p, kb in ((B.params(k=k, sink=sink, window=window), lambda m: k),
+                  (B.params(k_num=1, k_den=7, sink=sink, window=window), lambda m: m // 7)):
+        got = run_select(kv, bounds, qd, p, bs, n, hkv, batch, spare=3)
+        check_select(got, sigma, lens, hkv, kb, sink, window, bs)
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_block_select_ties_nan_and_lost_pages(paged):
+    # equal scores everywhere: the lowest blocks; a block of NaN bounds and one on
+    # a page outside the pool rank last
+    n, bs, d, hkv = 2000, 16, 64, 2
+    nb = -(-n // bs)
+    lens = (n, n - 5)
+    table = np.arange(2 * nb).reshape(2, nb)
+    K = torch.zeros((2 * nb, hkv, bs, d) if paged else (2, hkv, nb * bs, d), dtype=torch.bfloat16, device=DEV)
+    dtab = torch.tensor(table, dtype=I32, device=DEV) if paged else None
+    kv = B.KV(K, K, torch.tensor(lens, dtype=I32, device=DEV), n, 4, dtab)
+    lo = torch.zeros((2 * nb, hkv, d) if paged else (2, hkv, nb, d), dtype=torch.bfloat16, device=DEV)
+    hi = lo.clone()
+    at = lambda b, g, j: (int(table[b, j]), g) if paged else (b, g, j)  # noqa: E731
+    sig = {(b, g): np.zeros(nb) for b in range(2) for g in range(hkv)}
+    for g in range(hkv):
+        hi[at(0, g, 3)][0] = math.nan
+        sig[0, g][3] = -math.inf
+        hi[at(1, g, 60)][5] = 2.0
+        sig[1, g][60] = 2.0
+        lo[at(1, g, 61)].fill_(-0.0)
+    if paged:
+        dtab[1, 5] = 2 * nb
+        for g in range(hkv):
+            sig[1, g][5] = -math.inf
+    q = torch.ones(2, 4, d, dtype=torch.bfloat16, device=DEV)
+    for k in (16, 160, 1600, 4000):
+        p = B.params(k=k, sink=0, window=0)
+        got = run_select(kv, B.BlockBounds(kv, lo, hi), q, p, bs, n, hkv, 2)
+        check_select(got, lambda b, g: sig[b, g], lens, hkv, lambda m: k, 0, 0, bs)
+
+
+# ---- together ----------------------------------------------------------------------
+
+def test_store_select_and_attend_as_a_decode_loop():
+    """A prompt and seven steps: store, a selection of blocks every third step,
+    attention over the set and the tokens since."""
+    batch, hq, hkv, d, bs, T, P = 2, 8, 2, 128, 16, 7, 150
+    s = Store(batch, hkv, d, bs, True, "bf16", P + T, seed=20)
+    c = s.c
+    c.hq = hq
+    kv = B.QuantKV(c.dev["k"], c.dev["v"], c.dsc["k"], c.dsc["v"], c.seq, P + T, hq, c.dtable)
+    c.kv = kv
+    grid = lambda x: (x.float() * 16).round().clamp(-255, 255).div(16).to(x.dtype)  # noqa: E731
+    s.bounds = B.BlockBounds(kv, s.dlo, s.dhi)
+    k, v = s.tokens(P, wide=1.0)
+    s.store(grid(k), v, new=[P, P - 37])
+    p = B.params(k=48, sink=4, window=20, refresh_every=3)
+    got = None
+    for j in range(T):
+        k, v = s.tokens(1, wide=1.0)
+        s.store(grid(k), v)
+        s.check()
+        q = grid(torch.tensor(np.random.default_rng(j).standard_normal((batch, hq, d)), dtype=torch.bfloat16))
+        c.q, c.lens = q.to(DEV), tuple(s.n)
+        if j % 3 == 0:
+            got = run_select(kv, s.bounds, c.q, p, bs, P + T, hkv, batch)
+            anchor, sets = c.seq.clone(), {}
+            for b, n in enumerate(s.n):
+                for g in range(hkv):
+                    ids = [c.block(b, g, i) for i in range(-(-n // bs))]
+                    sig = Q.block_scores(q[b, g * 4:(g + 1) * 4].double().numpy(), s.lo[ids], s.hi[ids])
+                    blocks = Q.choose_blocks(sig, Q.candidate_blocks(n, 4, 20, bs), 48, bs)
+                    sets[b, g] = Q.block_set(blocks, n, 4, 20, bs)
+                    assert got[2][b, g, : len(sets[b, g])].tolist() == sets[b, g]
+        y, lse = c.outputs()
+        cap = got[2].shape[2]
+        B.prhs_quant_reuse_decode_attn(kv, c.q, got[2], got[3], anchor, c.scale_q, y, lse, c.workspace(False, cap))
+        n0 = anchor.tolist()
+        c.check(y, lse, lambda b, g: sets[b, g] + list(range(n0[b], s.n[b])))
+
+
+def test_graph_replays_equal_the_eager_calls():
+    batch, hq, hkv, d, bs, n = 3, 8, 2, 64, 16, 3000
+    lens = (n, 1200, 65)
+    c = Cache(lens, hq, hkv, d, bs, True, "bf16", seed=30)
+    lo = torch.randn(c.pages, hkv, d, device=DEV).bfloat16()
+    bounds = B.BlockBounds(c.kv, lo, lo + 1)
+    p = B.params(k=256, sink=4, window=32)
+    kc, sc = B.prhs_max_blocks(p, bs, n), B.prhs_block_set_capacity(p, bs, n)
+    blk, st = (torch.zeros(batch, hkv, x, dtype=I32, device=DEV) for x in (kc, sc))
+    bl, sl = (torch.zeros(batch, hkv, dtype=I32, device=DEV) for _ in range(2))
+    wb = B.workspace(B.prhs_block_workspace_size(c.kv, bounds), DEV)
+    ws = B.workspace(max(B.prhs_workspace_size(B.PRHS_OP_QUANT_SPARSE_ATTN, c.kv, None, sc),
+                         B.prhs_workspace_size(B.PRHS_OP_QUANT_DENSE_ATTN, c.kv)), DEV)
+    k1, v1 = (torch.randn(batch, hkv, 1, d, device=DEV).bfloat16() for _ in "kv")
+    y, lse = c.outputs()
+    z, zse = c.outputs()
+
+    def step():
+        B.prhs_quant_store(c.kv, k1, v1, None, bounds)
+        B.prhs_block_select(c.kv, c.q, p, bounds, blk, bl, st, sl, wb)
+        B.prhs_quant_sparse_decode_attn(c.kv, c.q, st, sl, c.scale_q, y, lse, ws)
+        B.prhs_quant_dense_decode_attn(c.kv, c.q, c.scale_q, z, zse, ws)
+
+    state = [*c.dev.values(), *c.dsc.values(), lo, bounds._keep[1], blk, bl, st, sl, y, lse, z, zse]
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in state]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for _ in range(3):
+        for t in (blk, bl, st, sl, y, lse, z, zse):
+            t.zero_()
+        ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(state, want):
+            va, vb = (t.view(torch.uint8) if t.dtype == E4 else t for t in (a, b))
+            assert torch.equal(torch.nan_to_num(va.float()), torch.nan_to_num(vb.float()))
+        torch.randn(1000, device=DEV).sum().item()   # eager work between the replays
