@@ -122,7 +122,9 @@ _HOST_ENTRIES = [
     "prhs_select", "prhs_select_shared", "prhs_select_gated", "prhs_gate_select",
     "prhs_dilate_reuse", "prhs_sparse_decode_attn", "prhs_sparse_decode_attn_static",
     "prhs_reuse_decode_attn", "prhs_dense_decode_attn", "prhs_pool_decode_attn",
-    "prhs_prefill_attn", "prhs_schedule",
+    "prhs_prefill_attn", "prhs_schedule", "prhs_quant_store", "prhs_quant_sparse_decode_attn",
+    "prhs_quant_reuse_decode_attn", "prhs_quant_dense_decode_attn", "prhs_quant_pool_decode_attn",
+    "prhs_block_bounds", "prhs_block_select",
 ]
 
 
@@ -331,6 +333,7 @@ class KV:
             raise ValueError("seq_lens must have one entry per sequence")
         self.dtype = K.dtype
         self.device = K.device
+        self.geometry = _geometry(self.c)
 
     # shapes the entry points expect, from the descriptor
     @property
@@ -394,6 +397,7 @@ class QuantKV:
         self._keep = (K8, V8, k_scale, v_scale, seq_lens, block_table)
         self.dtype = dtype
         self.device = K8.device
+        self.geometry = _geometry(self.shape_c)
         self.block_size = bs
 
     @property
@@ -448,7 +452,7 @@ class BlockBounds:
         if k_min.shape[-1] != c.head_dim:
             raise ValueError(f"k_min must end with dim {c.head_dim}, got {tuple(k_min.shape)}")
         self._keep = (k_min, k_max)
-        self._of = _geometry(c)
+        self._of = kv.geometry
         self.bounds = PrhsBounds(bs, k_min.data_ptr(), k_max.data_ptr())
         self.block_size = bs
 
@@ -467,7 +471,7 @@ def _geometry(c):
 def _fits(kv, bounds):
     if not isinstance(bounds, BlockBounds):
         raise TypeError("bounds must be a BlockBounds")
-    if bounds._of != _geometry(_shape_of(kv)):
+    if bounds._of != kv.geometry:
         raise ValueError("bounds were made for a cache of another shape")
 
 
@@ -842,6 +846,15 @@ def _launch(kv, stream, entry, *args):
         check(entry(*args, ctypes.c_void_p(stream.cuda_stream)))
 
 
+def _fast(kv, kinds, stream, bounds=None):
+    """Whether a call on this cache may take the native marshalling: the cache
+    on the current GPU, the stream one of that GPU, the bounds made for it."""
+    return (_host is not None and type(kv) in kinds and kv.device.type == "cuda"
+            and torch._C._cuda_getDevice() == kv.device.index
+            and (stream is None or stream.device == kv.device)
+            and (bounds is None or (type(bounds) is BlockBounds and bounds._of == kv.geometry)))
+
+
 def _new_lens(kv, new_lens):
     if new_lens is not None:
         _need(new_lens, torch.int32, "new_lens", shape=(_shape_of(kv).batch,))
@@ -856,6 +869,12 @@ def prhs_quant_store(kv, k_new, v_new, new_lens=None, bounds=None, stream=None):
     """Stores the tokens k_new, v_new [B][Hkv][T][d] (kv.dtype) as the last
     new_lens[b] (all T by default) of the seq_lens[b] tokens of each sequence of
     the QuantKV kv, and updates the BlockBounds `bounds` of their blocks."""
+    if _fast(kv, (QuantKV,), stream, bounds):
+        addr, keep = (None, None) if bounds is None else (addressof(bounds.bounds), bounds._keep)
+        st = _host.quant_store(addressof(kv.quant), kv._keep, kv.device.index, k_new, v_new,
+                               new_lens, addr, keep, _handle(stream))
+        if st is not None:
+            return check(st)
     _quant(kv)
     _need(k_new, kv.dtype, "k_new", dims=4)
     _need(k_new, kv.dtype, "k_new", shape=kv.per_unit() + (k_new.shape[2], kv.shape_c.head_dim))
@@ -878,6 +897,11 @@ def _quant_attention(kv, q, out, lse, ws):
 
 def prhs_quant_sparse_decode_attn(kv, q, set_idx, set_len, scale, out, lse, ws, stream=None):
     """prhs_sparse_decode_attn over a QuantKV."""
+    if _fast(kv, (QuantKV,), stream):
+        st = _host.quant_sparse(addressof(kv.quant), kv._keep, kv.device.index, q, set_idx, set_len,
+                                scale, out, lse, ws, _handle(stream))
+        if st is not None:
+            return check(st)
     _quant_attention(kv, q, out, lse, ws)
     _sets(kv, set_idx, set_len)
     kv.check_device(q=q, set_idx=set_idx, set_len=set_len, out=out, lse=lse, ws=ws)
@@ -889,6 +913,11 @@ def prhs_quant_sparse_decode_attn(kv, q, set_idx, set_len, scale, out, lse, ws, 
 def prhs_quant_reuse_decode_attn(kv, q, set_idx, set_len, anchor_lens, scale, out, lse, ws,
                                  stream=None):
     """prhs_reuse_decode_attn over a QuantKV."""
+    if _fast(kv, (QuantKV,), stream):
+        st = _host.quant_reuse(addressof(kv.quant), kv._keep, kv.device.index, q, set_idx, set_len,
+                               anchor_lens, scale, out, lse, ws, _handle(stream))
+        if st is not None:
+            return check(st)
     _quant_attention(kv, q, out, lse, ws)
     _sets(kv, set_idx, set_len)
     _need(anchor_lens, torch.int32, "anchor_lens", shape=(kv.shape_c.batch,))
@@ -901,6 +930,11 @@ def prhs_quant_reuse_decode_attn(kv, q, set_idx, set_len, anchor_lens, scale, ou
 
 def prhs_quant_dense_decode_attn(kv, q, scale, out, lse, ws, stream=None):
     """prhs_dense_decode_attn over a QuantKV."""
+    if _fast(kv, (QuantKV,), stream):
+        st = _host.quant_dense(addressof(kv.quant), kv._keep, kv.device.index, q, scale, out, lse,
+                               ws, _handle(stream))
+        if st is not None:
+            return check(st)
     _quant_attention(kv, q, out, lse, ws)
     kv.check_device(q=q, out=out, lse=lse, ws=ws)
     _launch(kv, stream, lib().prhs_quant_dense_decode_attn, ctypes.byref(kv.quant), _ptr(q),
@@ -910,6 +944,13 @@ def prhs_quant_dense_decode_attn(kv, q, scale, out, lse, ws, stream=None):
 def prhs_quant_pool_decode_attn(kv, q, pool_idx, pool_len, unit_row, unit_tail, scale, out, lse, ws,
                                 stream=None, psaw=None, unit_gate=None, units_side=PRHS_UNITS_ALL):
     """prhs_pool_decode_attn over a QuantKV."""
+    if _fast(kv, (QuantKV,), stream) and (psaw is None or type(psaw) is PrhsPsaw):
+        st = _host.quant_pool(addressof(kv.quant), kv._keep, kv.device.index, q, pool_idx, pool_len,
+                              unit_row, unit_tail, unit_gate, units_side,
+                              None if psaw is None else addressof(psaw), scale, out, lse, ws,
+                              _handle(stream))
+        if st is not None:
+            return check(st)
     _quant_attention(kv, q, out, lse, ws)
     units = kv.shape_c.batch * kv.shape_c.num_kv_heads
     if units_side != PRHS_UNITS_ALL:
@@ -936,6 +977,12 @@ def prhs_block_bounds(kv, bounds, new_cap, new_lens=None, stream=None):
     """Makes the BlockBounds `bounds` of the KV kv anew for the blocks that hold
     one of the last new_lens[b] (at most, and by default, new_cap) tokens of
     each sequence."""
+    if _fast(kv, (KV,), stream, bounds) and bounds is not None:
+        st = _host.block_bounds(addressof(kv.c), kv._keep, kv.device.index,
+                                addressof(bounds.bounds), bounds._keep, new_cap, new_lens,
+                                _handle(stream))
+        if st is not None:
+            return check(st)
     if not isinstance(kv, KV):
         raise TypeError("kv must be a KV (prhs_quant_store keeps the bounds of a QuantKV)")
     _fits(kv, bounds)
@@ -965,6 +1012,13 @@ def prhs_block_select(kv, q, p, bounds, blk_idx, blk_len, set_idx, set_len, ws, 
     a KV or QuantKV, within the budget and around the sink and window of the
     params p: their indices blk_idx [B][Hkv][cap], and the set of sink, blocks
     and window for the attention calls."""
+    if (_fast(kv, (KV, QuantKV), stream, bounds) and bounds is not None
+            and type(p) is PrhsParams):
+        st = _host.block_select(addressof(_shape_of(kv)), kv._keep, kv.device.index, q, addressof(p),
+                                addressof(bounds.bounds), bounds._keep, blk_idx, blk_len, set_idx,
+                                set_len, ws, _handle(stream))
+        if st is not None:
+            return check(st)
     _q(kv, q, (KV, QuantKV))
     _fits(kv, bounds)
     _need(blk_idx, torch.int32, "blk_idx", dims=3)

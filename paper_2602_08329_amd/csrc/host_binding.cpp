@@ -30,6 +30,13 @@ struct Entries {
   decltype(&prhs_pool_decode_attn) pool;
   decltype(&prhs_prefill_attn) prefill;
   decltype(&prhs_schedule) schedule;
+  decltype(&prhs_quant_store) quant_store;
+  decltype(&prhs_quant_sparse_decode_attn) quant_sparse;
+  decltype(&prhs_quant_reuse_decode_attn) quant_reuse;
+  decltype(&prhs_quant_dense_decode_attn) quant_dense;
+  decltype(&prhs_quant_pool_decode_attn) quant_pool;
+  decltype(&prhs_block_bounds) block_bounds;
+  decltype(&prhs_block_select) block_select;
 } E;
 
 // A check that does not hold: the caller answers None.
@@ -262,7 +269,8 @@ PyObject* f_sparse(ARGS) {  // without a workspace (None): the static form
   });
 }
 
-PyObject* f_reuse(ARGS) {
+template <typename Kv, typename Fn>
+PyObject* attend_reuse(Fn fn, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 12, [&] {
     const Cache kv(a[0], a[1], a[2]);
     int cap;
@@ -273,11 +281,15 @@ PyObject* f_reuse(ARGS) {
     float *out = kv.out(a[8]), *lse = kv.lse(a[9]);
     void* ws = kv.ws(a[10], &wb);
     void* st = as_ptr<void>(a[11]);
-    return call([&] { return E.reuse(kv.c, q, si, sl, cap, al, scale, out, lse, ws, wb, st); });
+    return call([&] { return fn((const Kv*)kv.c, q, si, sl, cap, al, scale, out, lse, ws, wb, st); });
   });
 }
 
-PyObject* f_dense(ARGS) {
+PyObject* f_reuse(ARGS) { return attend_reuse<prhs_kv>(E.reuse, a, n); }
+PyObject* f_quant_reuse(ARGS) { return attend_reuse<prhs_quant_kv>(E.quant_reuse, a, n); }
+
+template <typename Kv, typename Fn>
+PyObject* attend_dense(Fn fn, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&] {
     const Cache kv(a[0], a[1], a[2]);
     size_t wb;
@@ -286,11 +298,15 @@ PyObject* f_dense(ARGS) {
     float *out = kv.out(a[5]), *lse = kv.lse(a[6]);
     void* ws = kv.ws(a[7], &wb);
     void* st = as_ptr<void>(a[8]);
-    return call([&] { return E.dense(kv.c, q, scale, out, lse, ws, wb, st); });
+    return call([&] { return fn((const Kv*)kv.c, q, scale, out, lse, ws, wb, st); });
   });
 }
 
-PyObject* f_pool(ARGS) {
+PyObject* f_dense(ARGS) { return attend_dense<prhs_kv>(E.dense, a, n); }
+PyObject* f_quant_dense(ARGS) { return attend_dense<prhs_quant_kv>(E.quant_dense, a, n); }
+
+template <typename Kv, typename Fn>
+PyObject* attend_pool(Fn fn, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 16, [&] {
     const Cache kv(a[0], a[1], a[2]);
     size_t wb;
@@ -314,10 +330,13 @@ PyObject* f_pool(ARGS) {
     void* st = as_ptr<void>(a[15]);
     const auto *pi = (const int32_t*)p.data_ptr(), *pn = (const int32_t*)pl.data_ptr();
     return call([&] {
-      return E.pool(kv.c, q, pi, pn, rows, cap, ur, ut, gate, side, ps, scale, out, lse, ws, wb, st);
+      return fn((const Kv*)kv.c, q, pi, pn, rows, cap, ur, ut, gate, side, ps, scale, out, lse, ws, wb, st);
     });
   });
 }
+
+PyObject* f_pool(ARGS) { return attend_pool<prhs_kv>(E.pool, a, n); }
+PyObject* f_quant_pool(ARGS) { return attend_pool<prhs_quant_kv>(E.quant_pool, a, n); }
 
 PyObject* f_prefill(ARGS) {
   return guarded(n, 9, [&] {
@@ -338,6 +357,79 @@ PyObject* f_prefill(ARGS) {
 PyObject* f_schedule(ARGS) {  // the library's answer, -1 included
   return guarded(n, 3, [&] {
     return PyLong_FromLong(E.schedule(as_i32(a[0]), as_i32(a[1]), as_ptr<prhs_params>(a[2])));
+  });
+}
+
+// ---- 8-bit cache (a prhs_quant_kv begins with its prhs_kv) and blocks ----
+
+// A cache's bounds: their descriptor, and their tensors, which must still be on
+// its GPU (that they fit the cache's shape is checked in Python).
+const prhs_bounds* bounds_of(const Cache& kv, PyObject* addr, PyObject* keep) {
+  const auto* b = as_ptr<prhs_bounds>(addr);
+  if (b) {
+    need(PyTuple_CheckExact(keep));
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(keep); ++i) tensor(PyTuple_GET_ITEM(keep, i), kv.dev);
+  }
+  return b;
+}
+
+PyObject* f_quant_sparse(ARGS) {
+  return guarded(n, 11, [&] {
+    const Cache kv(a[0], a[1], a[2]);
+    int cap;
+    size_t wb;
+    const void* q = kv.q(a[3]);
+    const int32_t *si = kv.rows(a[4], &cap), *sl = kv.units(a[5]);
+    const float scale = (float)as_double(a[6]);
+    float *out = kv.out(a[7]), *lse = kv.lse(a[8]);
+    void* ws = kv.ws(a[9], &wb);
+    void* st = as_ptr<void>(a[10]);
+    return call([&] {
+      return E.quant_sparse((const prhs_quant_kv*)kv.c, q, si, sl, cap, scale, out, lse, ws, wb, st);
+    });
+  });
+}
+
+PyObject* f_quant_store(ARGS) {
+  return guarded(n, 9, [&] {
+    const Cache kv(a[0], a[1], a[2]);
+    const at::Tensor& t = tensor(a[3], kv.dev);
+    need(t.dim() == 4 && t.size(2) <= INT32_MAX);
+    const int64_t T = t.size(2);
+    const void* k = data<void>(a[3], kv.dtype, {kv.b, kv.hkv, T, kv.d}, kv.dev);
+    const void* v = data<void>(a[4], kv.dtype, {kv.b, kv.hkv, T, kv.d}, kv.dev);
+    const int32_t* lens = a[5] == Py_None ? nullptr : kv.lens(a[5]);
+    const prhs_bounds* bounds = bounds_of(kv, a[6], a[7]);
+    void* st = as_ptr<void>(a[8]);
+    return call([&] {
+      return E.quant_store((const prhs_quant_kv*)kv.c, k, v, (int)T, lens, bounds, st);
+    });
+  });
+}
+
+PyObject* f_block_bounds(ARGS) {
+  return guarded(n, 8, [&] {
+    const Cache kv(a[0], a[1], a[2]);
+    const prhs_bounds* bounds = bounds_of(kv, a[3], a[4]);
+    const int cap = as_i32(a[5]);
+    const int32_t* lens = a[6] == Py_None ? nullptr : kv.lens(a[6]);
+    void* st = as_ptr<void>(a[7]);
+    return call([&] { return E.block_bounds(kv.c, bounds, cap, lens, st); });
+  });
+}
+
+PyObject* f_block_select(ARGS) {
+  return guarded(n, 13, [&] {
+    const Cache kv(a[0], a[1], a[2]);
+    int bcap, scap;
+    size_t wb;
+    const void* q = kv.q(a[3]);
+    const auto* p = as_ptr<prhs_params>(a[4]);
+    const prhs_bounds* bounds = bounds_of(kv, a[5], a[6]);
+    int32_t *bi = kv.rows(a[7], &bcap), *bl = kv.units(a[8]), *si = kv.rows(a[9], &scap), *sl = kv.units(a[10]);
+    void* ws = kv.ws(a[11], &wb);
+    void* st = as_ptr<void>(a[12]);
+    return call([&] { return E.block_select(kv.c, q, p, bounds, bi, bl, bcap, si, sl, scap, ws, wb, st); });
   });
 }
 
@@ -365,7 +457,8 @@ PyObject* f_bind(ARGS) {
 PyMethodDef methods[] = {
     FAST(bind), FAST(select), FAST(select_shared), FAST(select_gated), FAST(gate_select),
     FAST(dilate_reuse), FAST(sparse), FAST(reuse), FAST(dense), FAST(pool), FAST(prefill),
-    FAST(schedule), {nullptr, nullptr, 0, nullptr}};
+    FAST(schedule), FAST(quant_store), FAST(quant_sparse), FAST(quant_reuse), FAST(quant_dense),
+    FAST(quant_pool), FAST(block_bounds), FAST(block_select), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_prhs_host", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
