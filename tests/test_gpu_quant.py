@@ -537,6 +537,39 @@ def test_block_select(hq, hkv, d, bs, paged, n, k, sink, window, dtype):
         check_select(got, sigma, lens, hkv, kb, sink, window, bs)
 
 
+@pytest.mark.parametrize("batch,hkv,nb,k,paged,dtype", [
+    (1, 2, 8750, 900, True, "bf16"),       # more keys than the picking workgroup's registers hold
+    (2, 1, 9000, 80000, False, "f32"),     # more chosen blocks than its LDS holds
+    (24, 8, 4300, 3000, False, "bf16"),    # one launch of long rows
+    (96, 1, 300, 640, True, "bf16"), (96, 1, 600, 640, False, "f32"), (10, 32, 200, 640, False, "bf16"),
+])
+def test_block_select_long_and_many_rows(batch, hkv, nb, k, paged, dtype):
+    bs, d, hq, n = 16, 64, hkv * 2, nb * 16 - 3
+    rng = np.random.default_rng(nb)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    lens = tuple(n - (b * 977) % (n // 3) for b in range(batch))
+    blocks = batch * nb * hkv
+    table = rng.permutation(batch * nb).reshape(batch, nb)
+    shape = (batch * nb, hkv, bs, d) if paged else (batch, hkv, nb * bs, d)
+    K = torch.empty(shape, dtype=torch.uint8, device=DEV).view(E4)   # not read
+    sc = torch.ones(shape[:2] if paged else (batch, hkv, nb), device=DEV)
+    kv = B.QuantKV(K, K, sc, sc, torch.tensor(lens, dtype=I32, device=DEV), n, hq,
+                   torch.tensor(table, dtype=I32, device=DEV) if paged else None, dtype=dt)
+    g = torch.Generator(device=DEV).manual_seed(nb)
+    x = torch.randn(blocks, d, generator=g, device=DEV).mul_(16).round_().clamp_(-255, 200).div_(16)
+    lo = x.to(dt).view(*sc.shape, d)
+    hi = (x + 1.5).to(dt).view(*sc.shape, d)
+    q = np.clip(np.round(rng.standard_normal((batch, hq, d)) * 16), -255, 255) / 16
+    p = B.params(k=k, sink=20, window=40)
+    got = run_select(kv, B.BlockBounds(kv, lo, hi), torch.tensor(q, dtype=dt, device=DEV), p, bs, n, hkv, batch)
+    for b in sorted({0, batch // 2, batch - 1}):
+        for g_ in sorted({0, hkv - 1}):
+            ids = [int(table[b, j]) * hkv + g_ if paged else (b * hkv + g_) * nb + j for j in range(nb)]
+            a, z = (t.reshape(-1, d)[ids].double().cpu().numpy() for t in (lo, hi))
+            sig = Q.block_scores(q[b, 2 * g_:2 * g_ + 2], a, z)
+            check_select([t[b:b + 1, g_:g_ + 1] for t in got], lambda *_: sig, [lens[b]], 1, lambda m: k, 20, 40, bs)
+
+
 @pytest.mark.parametrize("paged", [False, True])
 def test_block_select_ties_nan_and_lost_pages(paged):
     # equal scores everywhere: the lowest blocks; a block of NaN bounds and one on
