@@ -44,10 +44,11 @@ FLAGS = [
 ]
 
 
-# Per-source flags.  prefill.hip: MFMA accumulators in ordinary VGPRs; with
+# Per-source flags.  prefill.hip, quant_attention.hip: MFMA accumulators in ordinary VGPRs; with
 # the online-softmax rescale of the accumulators in its loop, the default
 # (accumulation registers) costs register copies on every key tile.
-EXTRA_FLAGS = {"prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA_FLAGS = {"prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "quant_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def hipcc():

@@ -269,7 +269,7 @@ prhs_status prhs_workspace_size(int32_t op, const prhs_kv* kv, const prhs_params
       if (st != PRHS_OK) return st;
       const bool dense = op == PRHS_OP_QUANT_DENSE_ATTN;
       if (!dense && set_cap < 0) return fail(PRHS_E_INVALID, "set_cap must be >= 0");
-      *bytes = prhs::quant_attn_workspace_bytes(dense, kv->batch, kv->num_q_heads, kv->num_kv_heads,
+      *bytes = prhs::quant_attn_workspace_bytes(kv->batch, kv->num_q_heads, kv->num_kv_heads,
                                                 kv->head_dim, dense ? kv->max_seq_len : set_cap);
       return PRHS_OK;
     }
@@ -418,11 +418,10 @@ static prhs_status attention_common(const prhs_kv* kv, const prhs::QuantScales* 
   if (psaw && (st = psaw_factor(psaw, &psaw_f)) != PRHS_OK) return st;
   const int rows_cap = dense ? kv->max_seq_len : set_cap;
   if (scales && (st = check_grid(std::max((long long)kv->batch * kv->num_q_heads,
-                                          prhs::quant_attn_groups(dense, kv->batch, kv->num_kv_heads,
-                                                                  rows_cap)))) != PRHS_OK)
+                                          prhs::quant_attn_groups(kv->batch, kv->num_kv_heads, rows_cap)))) != PRHS_OK)
     return st;
   const size_t wsz =
-      scales ? prhs::quant_attn_call_bytes(dense, kv->batch, kv->num_q_heads, kv->num_kv_heads,
+      scales ? prhs::quant_attn_call_bytes(kv->batch, kv->num_q_heads, kv->num_kv_heads,
                                            kv->head_dim, rows_cap)
              : prhs::attn_call_bytes(kv->dtype, dense, kv->batch, kv->num_q_heads,
                                      kv->num_kv_heads, kv->head_dim, rows_cap);

@@ -382,9 +382,9 @@ struct QuantScales {
   const float* v;
   int block_shift;
 };
-long long quant_attn_groups(bool dense, int batch, int hkv, int rows_cap);   // workgroups
-size_t quant_attn_call_bytes(bool dense, int batch, int hq, int hkv, int d, int rows_cap);
-size_t quant_attn_workspace_bytes(bool dense, int batch, int hq, int hkv, int d, int rows_cap);
+long long quant_attn_groups(int batch, int hkv, int rows_cap);   // workgroups
+size_t quant_attn_call_bytes(int batch, int hq, int hkv, int d, int rows_cap);
+size_t quant_attn_workspace_bytes(int batch, int hq, int hkv, int d, int rows_cap);
 hipError_t launch_quant_attention(const AttnLaunch& a, const QuantScales& scales, bool dense,
                                   hipStream_t stream);
 

@@ -6,15 +6,21 @@
 //
 // e4m3 values are exact in bf16 and fp16, so both products run on MFMA without
 // rounding an operand: K as bf16 with q (fp32 queries as three bf16 parts), V as
-// fp16 with the weights w_i = p_i vs_i 128 / R, R the largest vs of the chunk.
-// p stays below 2^8 (lazy rescaling), so w is at most 2^15, and as an fp16 pair
-// hi + lo it keeps 22 bits, or an absolute 2^-25: 2^-32 of the largest weight.
+// fp16 with the weights w_i = p_i vs_i r, r a power of two that brings the
+// largest vs the wave has met to at most 2^7.  p stays below 2^8 (lazy
+// rescaling), so w is below 2^15, and as an fp16 pair hi + lo it keeps 22 bits,
+// or an absolute 2^-25: 2^-32 of the largest weight.  With at most 8 heads a kv
+// head, hi and lo are two columns of one product (the queries stand in the
+// columns twice), else two products.
 //
-// Row ids and scales of the chunk are staged in LDS (a row's scale is that of
-// block row_id / block_size).  A wave then walks 32-row tiles, the next tile's
-// loads in flight while one is multiplied: K in whole rows (d / 16 lanes of 16
-// bytes) through a per-wave LDS tile into operand order, V (rows 16s + 4 grp + e,
-// d / 16 bytes per lane) straight into operands by byte permutes.
+// A wave walks tiles of 32 rows: lane l knows row l of its tile.  List entries
+// are read three tiles ahead, their pages two, K, V and scales one, into
+// registers in whole rows (d / 16 lanes of 16 bytes).  A tile passes through the
+// wave's own LDS, K into operand order, V by transposing reads
+// (ds_read_b64_tr_b8: of the 8-byte pieces that a group of 16 lanes addresses,
+// lane l receives byte l mod 8 of pieces l / 8, l / 8 + 2, ..).  Every load is
+// issued unconditionally, from a stand-in address where there is no row, as one
+// behind a branch would make the compiler wait for all of them.
 #include <algorithm>
 
 #include "attention_common.h"
@@ -28,109 +34,112 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_a2_t __attribute__((ext_vector_type(4), aligned(2)));
 
 struct QuantArgs : AttnArgs {
   QuantScales sc;
 };
 
-constexpr int kWaves = 4;
-constexpr int kMaxChunk = 64 * kWaves * kRowsPerThread;   // rows a workgroup stages
-constexpr long long kGroups = 256;                        // workgroups aimed at
-constexpr int kNoSplitRows = 512;
+constexpr int kTile = 32;   // rows of a wave's tile
 
-// LDS bytes of a wave: its K tile of 32 rows, at the end its G output rows.
+// LDS bytes of a wave: its tile of K, of V and their scales, at the end its G
+// output rows.
 __host__ __device__ constexpr int wave_bytes(int D, int G) {
-  return ((32 * D > G * (D + 1) * 4 ? 32 * D : G * (D + 1) * 4) + 15) & ~15;
+  const int tile = 2 * kTile * D + 2 * kTile * 4, out = G * (D + 1) * 4;
+  return ((tile > out ? tile : out) + 15) & ~15;
 }
 
-// 16-byte chunk c of tile row r in the wave's K tile.
+// LDS bytes of the query operands, which fp32 queries keep there.
+__host__ __device__ constexpr int query_bytes(int D, int QP) {
+  return QP > 1 ? QP * (D / 32) * 64 * 16 : 0;
+}
+
+// 16-byte chunk c of tile row r: the same chunk of eight rows lies in eight
+// different places of a 128-byte line.
 template <int D>
-__device__ __forceinline__ int kst_slot(int r, int c) {
-  constexpr int CH = D / 16;
-  return r * CH + (c ^ (r & (CH - 1)));
+__device__ __forceinline__ int tile_slot(int r, int c) {
+  return D == 128 ? r * 8 + (c ^ (r & 7)) : r * 4 + (c ^ ((r >> 1) & 3));
 }
 
-// Stages row ids and scales of list entries [start, start + n), and entries
-// without a row up to the next multiple of 32.  Scales of K carry the softmax
-// scale, those of V 128 / R; returns R / 128.
+// A unit's list in tiles: row ids of entry `t` in three steps, each from what the
+// one before loaded.
 template <bool DENSE, bool PAGED>
-__device__ __forceinline__ float stage(const QuantArgs& a, const int32_t (&raw)[kRowsPerThread],
-                                       int start, int n, const UnitSpan& sp, int nb, int b, int g,
-                                       int32_t* s_row, float* s_ks, float* s_vs, float* s_max) {
-  const int n32 = (n + 31) & ~31;
-  int pos[kRowsPerThread], row[kRowsPerThread];
-  float ks[kRowsPerThread], vs[kRowsPerThread];
-  entry_positions<DENSE>(raw, start, n, sp, pos);
-#pragma unroll
-  for (int k = 0; k < kRowsPerThread; ++k) row[k] = phys_row<PAGED>(a.kv, b, g, pos[k], nb);
-  float top = 0.f;
-#pragma unroll
-  for (int k = 0; k < kRowsPerThread; ++k) {
-    const int blk = row[k] < 0 ? 0 : row[k] >> a.sc.block_shift;
-    ks[k] = row[k] < 0 ? 0.f : a.sc.k[blk] * a.scale_log2;
-    vs[k] = row[k] < 0 ? 0.f : a.sc.v[blk];
-    top = fmaxf(top, vs[k]);
-  }
-  top = wave_max(top);
-  if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = top;
-  __syncthreads();
-  const int nwaves = blockDim.x >> 6;
-  for (int w = 0; w < nwaves; ++w) top = fmaxf(top, s_max[w]);
-  if (!(top > 0.f)) top = 1.f;
-  const float inv = 128.f / top;
-#pragma unroll
-  for (int k = 0; k < kRowsPerThread; ++k) {
-    const int r = threadIdx.x + k * blockDim.x;
-    if (r < n32) {
-      s_row[r] = row[k];
-      s_ks[r] = ks[k];
-      s_vs[r] = vs[k] * inv;
-    }
-  }
-  __syncthreads();
-  return top * (1.f / 128.f);
-}
+struct Rows {
+  const int32_t* idx;     // the unit's set
+  const int32_t* table;   // its sequence's pages
+  UnitSpan sp;
+  int nb, base, last_page, hkv, g, num_pages, shift, set_last;
 
-template <int D>
-struct Tile {
-  static constexpr int KL = D / 32;   // K loads of 16 bytes per lane
-  static constexpr int VW = D / 64;   // words of a V piece
-  u32x4_t k[KL];
-  uint32_t v[8][VW];
-  uint32_t ok;
+  __device__ __forceinline__ int entry(int t) const { return DENSE ? t : idx[min(t, set_last)]; }
+  // position of entry t, -1 for none; end: entries of the list
+  __device__ __forceinline__ int pos(int raw, int t, int end) const {
+    if (DENSE) return t < end ? t : -1;
+    int p = t < sp.base ? (raw < sp.t0 ? raw : -1) : sp.t0 + (t - sp.base);
+    if (p >= sp.mask_lo && p < sp.mask_hi) p = -1;
+    return t < end && p >= 0 && p < nb ? p : -1;
+  }
+  __device__ __forceinline__ int page(int p) const {
+    return PAGED ? table[min(max(p, 0) >> shift, last_page)] : 0;
+  }
+  __device__ __forceinline__ int row(int page, int p) const {
+    if (p < 0) return -1;
+    if (!PAGED) return base + p;
+    if (page < 0 || page >= num_pages || (p >> shift) > last_page) return -1;
+    return ((page * hkv + g) << shift) + (p & ((1 << shift) - 1));
+  }
 };
 
 template <int D>
-__device__ __forceinline__ void load_tile(Tile<D>& T, const int32_t* s_row, int r0, const uint8_t* kb,
-                                          const uint8_t* vb, int lane) {
+struct Tile {
+  static constexpr int KL = D / 32;   // loads of 16 bytes per lane, of K and of V
+  u32x4_t k[KL], v[KL];
+  float ks, vs;   // of row lane mod 32; 0 without a row
+  uint32_t ok;    // rows that are there
+};
+
+// Issues the loads of the tile whose row ids the lanes hold.
+template <int D>
+__device__ __forceinline__ void load_tile(Tile<D>& T, const QuantArgs& a, int row, int lane) {
   constexpr int CH = D / 16, RPI = 64 / CH;
-  const int col = lane & 15, grp = lane >> 4;
-  int rk[Tile<D>::KL], rv[8];
+  const uint8_t* kb = (const uint8_t*)a.kv.k;
+  const uint8_t* vb = (const uint8_t*)a.kv.v;
+  const int r0 = max(row, 0), blk = r0 >> a.sc.block_shift;
+  T.ok = (uint32_t)__builtin_amdgcn_ballot_w64(row >= 0);
+  T.ks = a.sc.k[blk];
+  T.vs = a.sc.v[blk];
 #pragma unroll
-  for (int j = 0; j < Tile<D>::KL; ++j) rk[j] = s_row[r0 + j * RPI + lane / CH];
+  for (int j = 0; j < Tile<D>::KL; ++j) {
+    const int64_t at = (int64_t)__shfl(r0, j * RPI + lane / CH) * D + (lane % CH) * 16;
+    T.k[j] = stream_load16(kb + at);
+    T.v[j] = stream_load16(vb + at);
+  }
+}
+
+// A loaded tile to the wave's LDS; rows that are not there get V = 0 and scales
+// of 0 (their K only reaches logits that are masked).
+template <int D>
+__device__ __forceinline__ void stage_tile(const Tile<D>& T, float scale_log2, u32x4_t* s_k, u32x4_t* s_v,
+                                           float* s_sc, int lane) {
+  constexpr int CH = D / 16, RPI = 64 / CH;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) rv[j] = s_row[r0 + 16 * (j >> 2) + grp * 4 + (j & 3)];
-#pragma unroll
-  for (int j = 0; j < Tile<D>::KL; ++j)
-    T.k[j] = stream_load16(kb + (int64_t)max(rk[j], 0) * D + (lane % CH) * 16);
-  T.ok = 0u;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint8_t* p = vb + (int64_t)max(rv[j], 0) * D + col * (D / 16);
-    if constexpr (D == 128) {
-      const u32x2_t x = stream_load8(p);
-      T.v[j][0] = x[0];
-      T.v[j][1] = x[1];
-    } else {
-      T.v[j][0] = __builtin_nontemporal_load((const uint32_t*)p);
-    }
-    if (rv[j] >= 0) T.ok |= 1u << j;
+  for (int j = 0; j < Tile<D>::KL; ++j) {
+    const int r = j * RPI + lane / CH, slot = tile_slot<D>(r, lane % CH);
+    s_k[slot] = T.k[j];
+    s_v[slot] = T.ok == 0xFFFFFFFFu || ((T.ok >> r) & 1u) ? T.v[j] : u32x4_t{0u, 0u, 0u, 0u};
+  }
+  if (lane < kTile) {
+    const bool in = (T.ok >> lane) & 1u;
+    s_sc[lane] = in ? T.ks * scale_log2 : 0.f;
+    s_sc[kTile + lane] = in ? T.vs : 0.f;
   }
 }
 
 template <int D>
 struct WaveState {
   float m, l;
+  int ve;       // exponent bits of the largest V scale met
+  float r;      // 2^(6 - that exponent)
   f32x4_t o[D / 16];
 };
 
@@ -143,59 +152,75 @@ __device__ __forceinline__ bf16x8_t bf16_of_e4m3(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
-template <bool HI>
-__device__ __forceinline__ uint32_t f16_of_e4m3(uint32_t a) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, HI));
+__device__ __forceinline__ f16x8_t f16_of_e4m3(uint32_t a, uint32_t b) {
+  uint32_t w[4];
+  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false));
+  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true));
+  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false));
+  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true));
+  return __builtin_bit_cast(f16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
-template <int D, int QP>
-__device__ __forceinline__ void consume_tile(Tile<D>& T, WaveState<D>& st,
-                                             const bf16x8_t (&qf)[QP][D / 32], const float* s_ks,
-                                             const float* s_vs, int r0, u32x4_t* kst, int lane) {
-  constexpr int CH = D / 16, RPI = 64 / CH;
+// Maximum over all 64 lanes of non-negative numbers' bits, in every lane.
+__device__ __forceinline__ int wave_imax(int v) {
+#define PRHS_ROR_IMAX(CTRL) v = max(v, __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false))
+  PRHS_ROR_IMAX(0x128);
+  PRHS_ROR_IMAX(0x124);
+  PRHS_ROR_IMAX(0x122);
+  PRHS_ROR_IMAX(0x121);
+#undef PRHS_ROR_IMAX
+  const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = max((int)a[0], (int)a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  return max((int)b[0], (int)b[1]);
+}
+
+// Lane (col, grp) owns query head col (with !WIDE col mod 8) and in the V product
+// the rows 16 s + 4 grp + e of the tile, in the order 4 s + e.
+template <int D, int QP, bool WIDE>
+__device__ __forceinline__ void consume_tile(uint32_t ok, WaveState<D>& st,
+                                             const bf16x8_t (&qf)[D / 32], const u32x4_t* s_q,
+                                             const u32x4_t* s_k, const u32x4_t* s_v, const float* s_sc,
+                                             int lane) {
+  constexpr int CH = D / 16;
   const int col = lane & 15, grp = lane >> 4;
-  // K to operand order: lane (col, grp) takes dims grp D/4 .. of rows col and 16 + col
-#pragma unroll
-  for (int j = 0; j < Tile<D>::KL; ++j) kst[kst_slot<D>(j * RPI + lane / CH, lane % CH)] = T.k[j];
-  __builtin_amdgcn_wave_barrier();
-  u32x4_t kr[2][CH / 4];
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int i = 0; i < CH / 4; ++i) kr[s][i] = kst[kst_slot<D>(16 * s + col, grp * (CH / 4) + i)];
-  __builtin_amdgcn_wave_barrier();
-  float x[8], w[8];
+  // lane (col, grp) takes dims grp D/4 .. of rows col and 16 + col
+  float x[8];
   float mt = -INFINITY;
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) {
-      const u32x4_t c = kr[s][kk >> 1];
-      const bf16x8_t kf = bf16_of_e4m3(c[2 * (kk & 1)], c[2 * (kk & 1) + 1]);
+    for (int i = 0; i < CH / 4; ++i) {
+      const u32x4_t c = s_k[tile_slot<D>(16 * s + col, grp * (CH / 4) + i)];
 #pragma unroll
-      for (int part = QP - 1; part >= 0; --part)   // small parts first
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[part][kk], acc, 0, 0, 0);
+      for (int h = 0; h < 2; ++h) {
+        const int kk = 2 * i + h;
+        const bf16x8_t kf = bf16_of_e4m3(c[2 * h], c[2 * h + 1]);
+        if constexpr (QP == 1) {
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[kk], acc, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int part = QP - 1; part >= 0; --part)   // small parts first
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                kf, __builtin_bit_cast(bf16x8_t, s_q[(part * (D / 32) + kk) * 64 + lane]), acc, 0, 0, 0);
+        }
+      }
     }
-    const float4 ks = *(const float4*)(s_ks + r0 + 16 * s + 4 * grp);
+    const float4 ks = *(const float4*)(s_sc + 16 * s + 4 * grp);
     const float kse[4] = {ks.x, ks.y, ks.z, ks.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = s * 4 + e;
-      x[j] = (T.ok >> j) & 1u ? acc[e] * kse[e] : -INFINITY;
-      mt = fmaxf(mt, x[j]);
-    }
+    for (int e = 0; e < 4; ++e) x[s * 4 + e] = acc[e] * kse[e];
   }
-  // entries without a row read a stand-in row: their V must not count
-  if (__builtin_amdgcn_ballot_w64(T.ok != 0xFFu)) {
+  if (ok != 0xFFFFFFFFu) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (!((T.ok >> j) & 1u)) {
-#pragma unroll
-        for (int i = 0; i < Tile<D>::VW; ++i) T.v[j][i] = 0u;
-      }
+    for (int j = 0; j < 8; ++j) x[j] = (ok >> (16 * (j >> 2) + 4 * grp + (j & 3))) & 1u ? x[j] : -INFINITY;
   }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) mt = fmaxf(mt, x[j]);
   mt = max_over_groups(mt);
+  // lazy rescaling: the reference st.m moves only when some head of the wave sees
+  // its maximum rise by more than 2^8
   const float m_new = fmaxf(st.m, mt);
   if (__builtin_amdgcn_ballot_w64(m_new > st.m + 8.f)) {
     const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
@@ -205,16 +230,16 @@ __device__ __forceinline__ void consume_tile(Tile<D>& T, WaveState<D>& st,
     for (int blk = 0; blk < D / 16; ++blk) st.o[blk] *= alpha;
   }
   const float mref = st.m == -INFINITY ? 0.f : st.m;
+  float w[8];
+  float4 vs[2];
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const float4 vs = *(const float4*)(s_vs + r0 + 16 * s + 4 * grp);
-    const float vse[4] = {vs.x, vs.y, vs.z, vs.w};
+  for (int s = 0; s < 2; ++s) vs[s] = *(const float4*)(s_sc + kTile + 16 * s + 4 * grp);
+  const float vse[8] = {vs[0].x, vs[0].y, vs[0].z, vs[0].w, vs[1].x, vs[1].y, vs[1].z, vs[1].w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float p = __builtin_amdgcn_exp2f(x[s * 4 + e] - mref);
-      st.l += p;
-      w[s * 4 + e] = p * vse[e];
-    }
+  for (int j = 0; j < 8; ++j) {
+    const float p = __builtin_amdgcn_exp2f(x[j] - mref);
+    st.l += p;
+    w[j] = p * (vse[j] * st.r);
   }
   uint32_t hi[4], lo[4];
 #pragma unroll
@@ -223,41 +248,34 @@ __device__ __forceinline__ void consume_tile(Tile<D>& T, WaveState<D>& st,
     hi[i] = __builtin_bit_cast(uint32_t, h);
     lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
         f32x2_t{w[2 * i] - (float)h[0], w[2 * i + 1] - (float)h[1]}, f16x2_t));
+    if (!WIDE) hi[i] = col < 8 ? hi[i] : lo[i];
   }
   const f16x8_t whi = __builtin_bit_cast(f16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
   const f16x8_t wlo = __builtin_bit_cast(f16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+  // lane `col` of a group addresses 8 dims of the group's row col / 2 (in the
+  // order of w) and receives dim 16 blk + col of its 8 rows
+  const int vr = 16 * (col >> 3) + 4 * grp + ((col >> 1) & 3);
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) {   // dims 2i, 2i + 1 of the lane's piece
-    uint32_t a0[4], a1[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      // bytes (row 2j, dim 2i), (row 2j+1, dim 2i), then the same of dim 2i + 1
-      const uint32_t y = __builtin_amdgcn_perm(T.v[2 * j + 1][i >> 1], T.v[2 * j][i >> 1],
-                                               (i & 1) ? 0x07030602u : 0x05010400u);
-      a0[j] = f16_of_e4m3<false>(y);
-      a1[j] = f16_of_e4m3<true>(y);
-    }
-    const f16x8_t v0 = __builtin_bit_cast(f16x8_t, make_uint4(a0[0], a0[1], a0[2], a0[3]));
-    const f16x8_t v1 = __builtin_bit_cast(f16x8_t, make_uint4(a1[0], a1[1], a1[2], a1[3]));
-    st.o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, whi, st.o[2 * i], 0, 0, 0);
-    st.o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, whi, st.o[2 * i + 1], 0, 0, 0);
-    st.o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, wlo, st.o[2 * i], 0, 0, 0);
-    st.o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, wlo, st.o[2 * i + 1], 0, 0, 0);
+  for (int blk = 0; blk < D / 16; ++blk) {
+    const uint8_t* at = (const uint8_t*)(s_v + tile_slot<D>(vr, blk)) + 8 * (col & 1);
+    const i32x2_t t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t*)at);
+    const f16x8_t v = f16_of_e4m3((uint32_t)t[0], (uint32_t)t[1]);
+    st.o[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, whi, st.o[blk], 0, 0, 0);
+    if (WIDE) st.o[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, wlo, st.o[blk], 0, 0, 0);
   }
 }
 
-// The query operand of product kk: dims grp D/4 + 8 kk .. +7 of head col, in QP
-// bf16 parts (fp32: the value is the sum of three, 24 bits).
-typedef uint32_t u32x4_a2_t __attribute__((ext_vector_type(4), aligned(2)));
+// The query operand of product kk: dims grp D/4 + 8 kk .. +7 of its head; fp32 in
+// three bf16 parts (24 bits), to LDS.
 template <int D, int QP>
-__device__ __forceinline__ void load_query(const void* q, size_t bh, bool on, int grp,
-                                           bf16x8_t (&qf)[QP][D / 32]) {
+__device__ __forceinline__ void load_query(const void* q, size_t bh, bool on, int grp, int lane,
+                                           bf16x8_t (&qf)[D / 32], u32x4_t* s_q) {
 #pragma unroll
   for (int kk = 0; kk < D / 32; ++kk) {
     const size_t at = bh * D + grp * (D / 4) + 8 * kk;
     if constexpr (QP == 1) {
       const u32x4_t v = *(const u32x4_a2_t*)((const __bf16*)q + at);
-      qf[0][kk] = __builtin_bit_cast(bf16x8_t, on ? v : u32x4_t{0u, 0u, 0u, 0u});
+      qf[kk] = __builtin_bit_cast(bf16x8_t, on ? v : u32x4_t{0u, 0u, 0u, 0u});
     } else {
       const float4 x = load_f32x4((const float*)q + at), y = load_f32x4((const float*)q + at + 4);
       float r[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
@@ -269,74 +287,117 @@ __device__ __forceinline__ void load_query(const void* q, size_t bh, bool on, in
           h[i] = (__bf16)(on ? r[i] : 0.f);
           r[i] -= (float)h[i];
         }
-        qf[part][kk] = h;
+        // every wave writes the same values
+        s_q[(part * (D / 32) + kk) * 64 + lane] = __builtin_bit_cast(u32x4_t, h);
       }
     }
   }
 }
 
-template <int D, bool DENSE, bool PAGED, int QP>
-__global__ __launch_bounds__(64 * kWaves) void quant_attn_split(QuantArgs a) {
-  // dynamic LDS: per-wave regions, then row ids and scales of the chunk
+template <int D, bool DENSE, bool PAGED, int QP, bool WIDE>
+__global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) {
+  // dynamic LDS: per-wave regions, then the query operands of fp32 queries
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
-  __shared__ float sm_m[kWaves][16], sm_l[kWaves][16], s_max[kWaves];
+  __shared__ float sm_m[kMaxWaves][16], sm_l[kMaxWaves][16];
   const int split = blockIdx.x % a.nsplit, u = blockIdx.x / a.nsplit;
   const int hkv = a.kv.hkv, hq = a.kv.hq, G = hq / hkv;
   const int wbytes = wave_bytes(D, G);
-  const int nwaves = blockDim.x >> 6, staged = blockDim.x * kRowsPerThread;
-  int32_t* s_row = (int32_t*)(dyn + (size_t)nwaves * wbytes);
-  float* s_ks = (float*)(s_row + staged);
-  float* s_vs = s_ks + staged;
+  const int nwaves = blockDim.x >> 6;
   const int b = u / hkv, g = u - b * hkv;
   const int start = split * a.chunk;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, grp = lane >> 4;
-  int32_t raw[kRowsPerThread];
-  prefetch_entries<DENSE>(a, u, start, raw);
-  bf16x8_t qf[QP][D / 32];
-  load_query<D, QP>(a.q, (size_t)b * hq + g * G + (col < G ? col : 0), col < G, grp, qf);
+  unsigned char* own = dyn + (size_t)wave * wbytes;
+  u32x4_t* s_k = (u32x4_t*)own;
+  u32x4_t* s_v = (u32x4_t*)(own + kTile * D);
+  float* s_sc = (float*)(own + 2 * kTile * D);
+  u32x4_t* s_q = (u32x4_t*)(dyn + (size_t)nwaves * wbytes);
+
+  // list entries, query and lengths load together
+  const int step = kTile * nwaves;
+  int t = start + wave * kTile + (lane & (kTile - 1));   // this lane's entry
+  Rows<DENSE, PAGED> rows;
+  if (!DENSE) {
+    int row = u;
+    if (a.unit_row) {
+      row = a.unit_row[u];
+      row = row >= 0 && row < a.pool_rows ? row : 0;
+    }
+    rows.idx = a.set_idx + (size_t)row * a.set_cap;
+    rows.set_last = max(a.set_cap, 1) - 1;
+  }
+  const bool any = DENSE || a.set_cap > 0;
+  int raw0 = any ? rows.entry(t) : -1, raw1 = any ? rows.entry(t + step) : -1,
+      raw2 = any ? rows.entry(t + 2 * step) : -1;
+  // a dense stream's first tile loads before the lengths are known: its positions
+  // are the cache's own, and those behind the length are masked below
+  rows.hkv = hkv;
+  rows.g = g;
+  rows.num_pages = a.kv.num_pages;
+  rows.shift = a.sc.block_shift;
+  rows.base = (b * hkv + g) * a.kv.capacity;
+  rows.table = PAGED ? a.kv.table + (int64_t)b * a.kv.max_pages : nullptr;
+  rows.last_page = a.kv.max_pages - 1;
+  Tile<D> T;
+  if (DENSE && a.kv.max_seq_len > 0) {
+    const int p = min(t, a.kv.max_seq_len - 1);
+    load_tile<D>(T, a, rows.row(rows.page(p), p), lane);
+  }
+  bf16x8_t qf[D / 32];
+  const int head = WIDE ? col : col & 7;
+  load_query<D, QP>(a.q, (size_t)b * hq + g * G + (head < G ? head : 0), head < G, grp, lane, qf, s_q);
   const int nb = kv_seq_len(a.kv, b);
   if (!DENSE && unit_excluded(a, u)) return;
-  const UnitSpan sp = unit_span<DENSE>(a, u, b, nb);
-  const int L = sp.L;
+  rows.sp = unit_span<DENSE>(a, u, b, nb);
+  const int L = rows.sp.L;
   if (L == 0 && split == 0) {  // empty set: y = 0, lse = -inf
     for (int e = threadIdx.x; e < G * D; e += blockDim.x)
       write_final(a, (size_t)b * hq + g * G + e / D, D, e % D, -INFINITY, 0.f, 0.f);
     return;
   }
   if (start >= L) return;
-  const int n = min(L, start + a.chunk) - start;
-  const float unscale = stage<DENSE, PAGED>(a, raw, start, n, sp, nb, b, g, s_row, s_ks, s_vs, s_max);
+  const int end = min(L, start + a.chunk);
+  rows.nb = nb;
 
-  const uint8_t* kb = (const uint8_t*)a.kv.k;
-  const uint8_t* vb = (const uint8_t*)a.kv.v;
   WaveState<D> st;
   st.m = -INFINITY;
   st.l = 0.f;
+  st.ve = 0;
+  st.r = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int ntiles = (n + 31) >> 5;
-  const int iters = wave < ntiles ? (ntiles - wave + nwaves - 1) / nwaves : 0;
+  const int ntiles = (end - start + kTile - 1) / kTile;
+  // (no page of an empty sequence is looked up: its table may be empty too)
+  const int iters = nb > 0 && wave < ntiles ? (ntiles - wave + nwaves - 1) / nwaves : 0;
   if (iters > 0) {
-    Tile<D> A, B;
-    u32x4_t* kst = (u32x4_t*)(dyn + (size_t)wave * wbytes);
-    const int step = 32 * nwaves;
-    int r0 = wave * 32;
-    load_tile<D>(A, s_row, r0, kb, vb, lane);
-    int i = 0;
-    for (; i + 2 < iters; i += 2) {
-      load_tile<D>(B, s_row, r0 + step, kb, vb, lane);
-      consume_tile<D, QP>(A, st, qf, s_ks, s_vs, r0, kst, lane);
-      load_tile<D>(A, s_row, r0 + 2 * step, kb, vb, lane);
-      consume_tile<D, QP>(B, st, qf, s_ks, s_vs, r0 + step, kst, lane);
-      r0 += 2 * step;
-    }
-    if (i + 1 < iters) {
-      load_tile<D>(B, s_row, r0 + step, kb, vb, lane);
-      consume_tile<D, QP>(A, st, qf, s_ks, s_vs, r0, kst, lane);
-      consume_tile<D, QP>(B, st, qf, s_ks, s_vs, r0 + step, kst, lane);
+    int p1 = rows.pos(raw1, t + step, end);
+    if (DENSE) {
+      T.ok &= (uint32_t)__builtin_amdgcn_ballot_w64(t < end);
     } else {
-      consume_tile<D, QP>(A, st, qf, s_ks, s_vs, r0, kst, lane);
+      const int p0 = rows.pos(raw0, t, end);
+      load_tile<D>(T, a, rows.row(rows.page(p0), p0), lane);
+    }
+    int g1 = rows.page(p1);
+    for (int i = 0; i < iters; ++i) {
+      const uint32_t ok = T.ok;
+      const int ve = max(wave_imax(__float_as_int((ok >> (lane & (kTile - 1))) & 1u ? T.vs : 0.f)) >> 23, 1);
+      __builtin_amdgcn_wave_barrier();
+      stage_tile<D>(T, a.scale_log2, s_k, s_v, s_sc, lane);
+      __builtin_amdgcn_wave_barrier();
+      load_tile<D>(T, a, rows.row(g1, p1), lane);
+      p1 = rows.pos(raw2, t + 2 * step, end);
+      g1 = rows.page(p1);
+      raw2 = any ? rows.entry(t + 3 * step) : -1;
+      t += step;
+      if (ve > st.ve) {   // a larger V scale than any before
+        const float r = __uint_as_float((uint32_t)min(max(260 - ve, 1), 253) << 23);
+        const float f = st.ve > 0 ? r / st.r : 1.f;
+        st.ve = ve;
+        st.r = r;
+#pragma unroll
+        for (int blk = 0; blk < D / 16; ++blk) st.o[blk] *= f;
+      }
+      consume_tile<D, QP, WIDE>(ok, st, qf, s_q, s_k, s_v, s_sc, lane);
     }
   }
 
@@ -345,13 +406,17 @@ __global__ __launch_bounds__(64 * kWaves) void quant_attn_split(QuantArgs a) {
     sm_m[wave][col] = st.m;
     sm_l[wave][col] = st.l;
   }
-  if (col < G) {
-    float* wo = (float*)(dyn + (size_t)wave * wbytes) + col * (D + 1);
+  const float unscale = st.r > 0.f ? 1.f / st.r : 0.f;
+  __builtin_amdgcn_wave_barrier();
+  float* wo = (float*)own + col * (D + 1);
 #pragma unroll
-    for (int blk = 0; blk < D / 16; ++blk)
+  for (int blk = 0; blk < D / 16; ++blk)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) wo[(grp * 4 + i) * (D / 16) + blk] = st.o[blk][i] * unscale;
-  }
+    for (int i = 0; i < 4; ++i) {
+      float v = st.o[blk][i] * unscale;
+      if (!WIDE) v = add_rotated<0x128>(v);   // hi and lo: columns 8 apart
+      if (col < G) wo[16 * blk + 4 * grp + i] = v;
+    }
   __syncthreads();
   const int nsp = (L + a.chunk - 1) / a.chunk;
   for (int e = threadIdx.x; e < G * D; e += blockDim.x) {
@@ -380,26 +445,62 @@ __global__ __launch_bounds__(64 * kWaves) void quant_attn_split(QuantArgs a) {
   }
 }
 
-// Rows per workgroup and splits per unit: at most kGroups workgroups, or as many
-// as staging needs.
-void split_geometry(bool dense, long long units, int rows_cap, int* chunk, int* nsplit) {
+// Splits of a unit and rows of a split, a multiple of the tile.  Times in us, d 128
+// with 4 heads a kv head where nothing else is said.
+// Up to 256 units: one workgroup per CU, but no split of few rows, which saves
+// the merge launch (8 units of 600 rows 9.9 whole, 11.6 in six; of 1200 17.3 and
+// 11.6; 96 units of 1200 rows 15.5 whole, 16.6 in two; of 2400 23.4 and 22.3), no
+// split below kMinSplit rows, and three of long rows where that leaves a third of
+// the CUs idle (160 units of 4096 rows 40.9 in three, 41.6 whole, at d 64 of 16384
+// 62.8 and 106; 200 units of 16384 rows 147.5 whole, 158 in six).
+// More units than CUs: whole, as the workgroups of a CU share it (512 of 16384 rows
+// 330, in two 338), but long rows of a few more units than CUs, which wait for the
+// CUs that take two (288 of 16384 rows 251 whole, 216 in four; 384 291 and 281).
+constexpr long long kCus = 256;
+constexpr int kWholeFew = 768, kWholeMany = 1536, kFewUnits = 64;
+constexpr int kMinSplit = 128;
+constexpr long long kThirdIdle = 176;
+constexpr int kLongRows = 3072;
+
+long long splits_of(long long units, long long rows) {
+  if (units > kCus) {
+    if (units <= 320 && rows >= kLongRows) return 4;
+    return units < 448 && rows >= 2 * kLongRows ? 2 : 1;
+  }
+  if (rows <= (units > kFewUnits ? kWholeMany : kWholeFew)) return 1;
+  const long long k = units > kCus / 2 && units <= kThirdIdle && rows >= kLongRows ? 3 : kCus / units;
+  return std::max(1LL, std::min(k, rows / kMinSplit));
+}
+
+void split_geometry(long long units, int rows_cap, int* chunk, int* nsplit) {
   const long long rows = std::max(rows_cap, 1);
-  const long long k = std::max(1LL, kGroups / std::max(1LL, units));
-  long long c = (rows + k - 1) / k;
-  if (!dense && rows <= kNoSplitRows) c = rows;
-  c = std::min<long long>((c + 31) / 32 * 32, kMaxChunk);
+  const long long k = splits_of(std::max(1LL, units), rows);
+  const long long c = ((rows + k - 1) / k + kTile - 1) / kTile * kTile;
   *chunk = (int)c;
   *nsplit = (int)((rows + c - 1) / c);
 }
 
-template <int D, bool DENSE, bool PAGED, int QP>
+// Waves of a workgroup, one for each tile at most: eight where it has a CU to
+// itself (8 units of 256 rows 7.8, with four 8.4, 256 of 4800 62.3 and 64.7) and for
+// long streams (1024 units of 16384 rows at d 64 323 and 338), else four (512 of
+// 600 rows 22.1, with eight 25.5).
+int waves_for(long long groups, int chunk) {
+  const int most = groups <= kCus || chunk > 8192 ? kMaxWaves : 4;
+  return std::min(most, chunk / kTile);
+}
+
+template <int D, bool DENSE, bool PAGED, int QP, bool WIDE>
 hipError_t launch_typed(const QuantArgs& a, hipStream_t stream) {
   const int units = a.kv.batch * a.kv.hkv, G = a.kv.hq / a.kv.hkv;
-  const int waves = std::min(kWaves, (a.chunk + 31) / 32);
-  const size_t dyn = (size_t)waves * (wave_bytes(D, G) + 64 * kRowsPerThread * 12);
-  static_assert(kWaves * (wave_bytes(D, 16) + 64 * kRowsPerThread * 12) <= 65536 - 1024,
-                "LDS that needs no attribute");
-  hipLaunchKernelGGL((quant_attn_split<D, DENSE, PAGED, QP>), dim3((unsigned)units * a.nsplit),
+  const int waves = waves_for((long long)units * a.nsplit, a.chunk);
+  const size_t dyn = (size_t)waves * wave_bytes(D, G) + query_bytes(D, QP);
+  if (dyn > 49152) {
+    const hipError_t e = hipFuncSetAttribute((const void*)quant_attn_split<D, DENSE, PAGED, QP, WIDE>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             kMaxWaves * wave_bytes(D, 16) + query_bytes(D, QP));
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((quant_attn_split<D, DENSE, PAGED, QP, WIDE>), dim3((unsigned)units * a.nsplit),
                      dim3(64 * waves), dyn, stream, a);
   if (a.nsplit > 1)
     hipLaunchKernelGGL((attn_merge<D, DENSE>), dim3(a.kv.batch * a.kv.hq), dim3(256), 0, stream,
@@ -407,38 +508,45 @@ hipError_t launch_typed(const QuantArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int D, bool DENSE, bool PAGED>
+hipError_t launch_query(const QuantArgs& a, int dtype, hipStream_t stream) {
+  if (a.kv.hq / a.kv.hkv > 8)
+    return dtype == 1 ? launch_typed<D, DENSE, PAGED, 1, true>(a, stream)
+                      : launch_typed<D, DENSE, PAGED, 3, true>(a, stream);
+  return dtype == 1 ? launch_typed<D, DENSE, PAGED, 1, false>(a, stream)
+                    : launch_typed<D, DENSE, PAGED, 3, false>(a, stream);
+}
+
 template <int D, bool DENSE>
 hipError_t launch_layout(const QuantArgs& a, int dtype, hipStream_t stream) {
-  if (a.kv.paged)
-    return dtype == 1 ? launch_typed<D, DENSE, true, 1>(a, stream)
-                      : launch_typed<D, DENSE, true, 3>(a, stream);
-  return dtype == 1 ? launch_typed<D, DENSE, false, 1>(a, stream)
-                    : launch_typed<D, DENSE, false, 3>(a, stream);
+  return a.kv.paged ? launch_query<D, DENSE, true>(a, dtype, stream)
+                    : launch_query<D, DENSE, false>(a, dtype, stream);
 }
 
 }  // namespace
 
-long long quant_attn_groups(bool dense, int batch, int hkv, int rows_cap) {
+long long quant_attn_groups(int batch, int hkv, int rows_cap) {
   int chunk, nsplit;
-  split_geometry(dense, (long long)batch * hkv, rows_cap, &chunk, &nsplit);
+  split_geometry((long long)batch * hkv, rows_cap, &chunk, &nsplit);
   return (long long)batch * hkv * nsplit;
 }
 
-size_t quant_attn_call_bytes(bool dense, int batch, int hq, int hkv, int d, int rows_cap) {
+size_t quant_attn_call_bytes(int batch, int hq, int hkv, int d, int rows_cap) {
   int chunk, nsplit;
-  split_geometry(dense, (long long)batch * hkv, rows_cap, &chunk, &nsplit);
+  split_geometry((long long)batch * hkv, rows_cap, &chunk, &nsplit);
   return attn_layout(batch, hq, d, nsplit).total;
 }
 
-// A call of fewer sequences may split its units more: a launch has at most
-// max(kGroups, units * the splits that staging needs) workgroups, so that many
-// partials of hq / hkv heads hold every such call.
-size_t quant_attn_workspace_bytes(bool dense, int batch, int hq, int hkv, int d, int rows_cap) {
-  const long long units = (long long)batch * hkv, rows = std::max(rows_cap, 1);
-  const long long groups = std::max(kGroups, units * ((rows + kMaxChunk - 1) / kMaxChunk));
+// A call of fewer sequences may split its units more: up to 256 units have at
+// most 3 x 176 splits in all, up to 320 four each and up to 447 two, all others
+// one, so that many partials of hq / hkv heads hold every smaller call.
+size_t quant_attn_workspace_bytes(int batch, int hq, int hkv, int d, int rows_cap) {
+  const long long units = (long long)batch * hkv;
+  const long long groups = std::max(units, units > kCus ? 4 * std::min(units, 320LL)
+                                                        : std::max(kCus, 3 * std::min(units, kThirdIdle)));
   const long long per = units > 0 ? (groups + units - 1) / units : 0;
   return std::max(attn_layout(batch, hq, d, (int)per).total,
-                  quant_attn_call_bytes(dense, batch, hq, hkv, d, rows_cap));
+                  quant_attn_call_bytes(batch, hq, hkv, d, rows_cap));
 }
 
 hipError_t launch_quant_attention(const AttnLaunch& s, const QuantScales& scales, bool dense,
@@ -460,8 +568,8 @@ hipError_t launch_quant_attention(const AttnLaunch& s, const QuantScales& scales
   a.psaw_sink = s.psaw_sink;
   a.set_cap = s.set_cap;
   a.scale_log2 = s.scale * 1.44269504088896340736f;
-  split_geometry(dense, (long long)s.kv.batch * s.kv.hkv, dense ? s.kv.max_seq_len : s.set_cap,
-                 &a.chunk, &a.nsplit);
+  split_geometry((long long)s.kv.batch * s.kv.hkv, dense ? s.kv.max_seq_len : s.set_cap, &a.chunk,
+                 &a.nsplit);
   const AttnLayout L = attn_layout(s.kv.batch, s.kv.hq, s.kv.d, a.nsplit);
   a.part_o = (float*)((char*)s.ws + L.part_o);
   a.part_ml = (float*)((char*)s.ws + L.part_ml);
