@@ -300,20 +300,6 @@ struct PickLds {
   uint32_t ncand, bin, left, count, key;
 };
 
-// Maximum over all 64 lanes, in every lane: rotations inside each row of 16
-// lanes, then across the rows.
-template <int CTRL>
-__device__ __forceinline__ uint32_t umax_rotated(uint32_t v) {
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false));
-}
-__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
-  v = umax_rotated<0x121>(umax_rotated<0x122>(umax_rotated<0x124>(umax_rotated<0x128>(v))));
-  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  v = max(a[0], a[1]);
-  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  return max(b[0], b[1]);
-}
-
 // A wave's share of a row's n keys, in order: rounds of 64, key 64 j + lane of
 // round j.  With R > 0 rounds they are in registers, else read from `keys`.
 template <int NT, int R>

@@ -1,6 +1,6 @@
 // The 8-bit KV cache's store, and the key bounds of blocks.
 //
-// quant_store: one workgroup per (kv head, block of tokens, K or V).  With s_old
+// quant_store: a team of waves per (kv head, block of tokens, K or V).  With s_old
 // the block's scale and amax the largest finite |x| of its new tokens,
 //   s_new = 2^e, e = max(-100, min {e : amax <= 448 * 2^e}),
 //   s = s_new if the block holds no earlier token, else max(s_old, s_new),
@@ -12,7 +12,7 @@
 // fall below 2^-6 s.  Since e4m3 is itself a floating type, a scale between two
 // powers of two would not make it more exact.
 //
-// A workgroup reads its new elements once, 8 per thread and step, holds them in
+// A team reads its new elements once, 8 per thread and step, holds them in
 // registers while their maximum is taken, and writes their bytes.  Bounds come
 // from the same registers.
 #include "prhs_internal.h"
@@ -109,83 +109,124 @@ __device__ __forceinline__ bool find_block(const KvView& kv, const NewTokens& to
   return true;
 }
 
-// Per-dimension minimum and maximum over a workgroup whose thread t holds those
-// of dims 8 (t mod D/8) .. +7 over its rows; thread t < D gets dim t's.
-template <int D>
-__device__ __forceinline__ void reduce_bounds(float (&mn)[8], float (&mx)[8], float* s_red, float* lo,
-                                              float* hi) {
-  constexpr int C = D / 8;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Minimum and maximum over the lanes that hold the same dims (lane mod C), in
+// every lane.
+template <int C>
+__device__ __forceinline__ void wave_bounds(float (&mn)[8], float (&mx)[8]) {
 #pragma unroll
-  for (int o = C; o < 64; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      mn[i] = fminf(mn[i], __shfl_xor(mn[i], o));
-      mx[i] = fmaxf(mx[i], __shfl_xor(mx[i], o));
+  for (int i = 0; i < 8; ++i) {
+    if (C == 8) {
+      mn[i] = fminf(mn[i], __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(mn[i]), 0x128, 0xF, 0xF, false)));
+      mx[i] = fmaxf(mx[i], __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(mx[i]), 0x128, 0xF, 0xF, false)));
     }
-  if (lane < C)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s_red[(wave * 2) * D + lane * 8 + i] = mn[i];
-      s_red[(wave * 2 + 1) * D + lane * 8 + i] = mx[i];
-    }
-  __syncthreads();
-  if (threadIdx.x < D) {
-    float a = INFINITY, z = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
-      a = fminf(a, s_red[(w * 2) * D + threadIdx.x]);
-      z = fmaxf(z, s_red[(w * 2 + 1) * D + threadIdx.x]);
-    }
-    *lo = a;
-    *hi = z;
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(mn[i]), __float_as_uint(mn[i]), false, false);
+    mn[i] = fminf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(mn[i]), __float_as_uint(mn[i]), false, false);
+    mn[i] = fminf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    const auto c = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx[i]), __float_as_uint(mx[i]), false, false);
+    mx[i] = fmaxf(__uint_as_float(c[0]), __uint_as_float(c[1]));
+    const auto d = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx[i]), __float_as_uint(mx[i]), false, false);
+    mx[i] = fmaxf(__uint_as_float(d[0]), __uint_as_float(d[1]));
   }
 }
 
-template <typename T, int D, int VPT>
-__global__ __launch_bounds__(kThreads) void quant_store(QuantStoreLaunch a, int nblk) {
+// The same over the W waves of a team, whose first C lanes get it; `lds` holds
+// 2 D floats for each wave of the workgroup.  All threads of the workgroup call it.
+template <int D, int W>
+__device__ __forceinline__ void team_bounds(float (&mn)[8], float (&mx)[8], float* lds) {
+  constexpr int C = D / 8;
+  wave_bounds<C>(mn, mx);
+  if (W == 1) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave / W * W;
+  if (lane < C)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      lds[(wave * 2) * D + lane * 8 + i] = mn[i];
+      lds[(wave * 2 + 1) * D + lane * 8 + i] = mx[i];
+    }
+  __syncthreads();
+  if (lane < C)
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        mn[i] = fminf(mn[i], lds[((first + w) * 2) * D + lane * 8 + i]);
+        mx[i] = fmaxf(mx[i], lds[((first + w) * 2 + 1) * D + lane * 8 + i]);
+      }
+}
+
+__device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
+  typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+  bf16x8_t v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
+  *(bf16x8_t*)p = v;
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
+  *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// A team of W waves per block, kThreads / (64 W) blocks a workgroup; thread t of
+// a team holds the elements 8 v .. 8 v + 7 of the block for v = t + 64 W i.  Rows
+// that are not new stand in for the nearest one that is, which changes neither the
+// maximum nor the bounds and keeps the loads free of branches.
+template <typename T, int D, int W, int VPT>
+__global__ __launch_bounds__(kThreads) void quant_store(QuantStoreLaunch a, int nblk, int blocks) {
   constexpr int C = D / 8;
   __shared__ uint32_t s_amax[kThreads / 64];
-  __shared__ float s_red[2 * (kThreads / 64) * D];
-  const int u = blockIdx.x / nblk;
+  __shared__ float s_red[W > 1 ? 2 * (kThreads / 64) * D : 1];
+  const int team = blockIdx.x * (kThreads / 64 / W) + (threadIdx.x >> 6) / W, tt = threadIdx.x & (64 * W - 1);
   const bool is_k = blockIdx.y == 0;
+  const int u = team / nblk;
   Block k;
-  if (!find_block(a.kv, a.tok, a.block_shift, u, blockIdx.x - u * nblk, &k)) return;
-  const int nold = k.lo - k.at, rows = k.hi - k.at;
-  const T* src = (const T*)(is_k ? a.k_new : a.v_new) +
-                 ((int64_t)(k.b * a.kv.hkv + k.g) * a.tok.cap + k.t0) * D;
-  uint8_t* dst = (uint8_t*)(is_k ? a.kv.k : a.kv.v) + (int64_t)k.row * D;
-  float* scale = (is_k ? a.k_scale : a.v_scale) + (k.row >> a.block_shift);
-
+  const bool on = team < blocks && find_block(a.kv, a.tok, a.block_shift, u, team - u * nblk, &k);
+  if (W == 1 && !on) return;
   float x[VPT][8];
   uint32_t amax = 0u;
+  int nold = 0, rows = 0;
+  uint8_t* dst = nullptr;
+  float* scale = nullptr;
+  float s_old = 0.f;
+  if (on) {
+    nold = k.lo - k.at;
+    rows = k.hi - k.at;
+    const T* src = (const T*)(is_k ? a.k_new : a.v_new) +
+                   ((int64_t)(k.b * a.kv.hkv + k.g) * a.tok.cap + k.t0) * D + (tt % C) * 8;
+    dst = (uint8_t*)(is_k ? a.kv.k : a.kv.v) + (int64_t)k.row * D + (tt % C) * 8;
+    scale = (is_k ? a.k_scale : a.v_scale) + (k.row >> a.block_shift);
+    s_old = *scale;
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int v = threadIdx.x + i * kThreads, r = v / C, c = v % C;
-    if (r < nold || r >= rows) continue;
-    load8(src + (int64_t)(r - nold) * D + c * 8, x[i]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t m = __float_as_uint(x[i][e]) & 0x7FFFFFFFu;
-      amax = max(amax, m < 0x7F800000u ? m : 0u);
+    for (int i = 0; i < VPT; ++i) {
+      const int r = (tt + i * 64 * W) / C;
+      load8(src + (int64_t)(min(max(r, nold), rows - 1) - nold) * D, x[i]);
     }
-  }
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o));
-  if ((threadIdx.x & 63) == 0) s_amax[threadIdx.x >> 6] = amax;
-  const float s_old = *scale;
-  __syncthreads();
-  amax = max(max(s_amax[0], s_amax[1]), max(s_amax[2], s_amax[3]));
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t m = __float_as_uint(x[i][e]) & 0x7FFFFFFFu;
+        amax = max(amax, m < 0x7F800000u ? m : 0u);
+      }
+  }
+  amax = wave_umax(amax);
+  if (W > 1) {
+    const int wave = threadIdx.x >> 6, first = wave / W * W;
+    if ((threadIdx.x & 63) == 0) s_amax[wave] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) amax = max(amax, s_amax[first + w]);
+  }
   const float s_new = __uint_as_float(scale_bits(amax));
   const bool grows = nold > 0 && !(s_old >= s_new);
   const float s = nold > 0 && !grows ? s_old : s_new;
-  const uint32_t sb = __float_as_uint(s);
-  const uint32_t se = sb >> 23;   // a positive power of two of which 2^-e is normal too
+  const uint32_t sb = __float_as_uint(s), se = sb >> 23;
+  // 1 / s where s and it are normal powers of two
   const float inv = (sb & 0x7FFFFFu) == 0u && se >= 1u && se <= 253u ? __uint_as_float((254u - se) << 23) : 0.f;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int v = threadIdx.x + i * kThreads, r = v / C, c = v % C;
-    u32x2_t* p = (u32x2_t*)(dst + (int64_t)r * D + c * 8);
+    const int r = (tt + i * 64 * W) / C;
+    u32x2_t* p = (u32x2_t*)(dst + (int64_t)r * D);
     if (r >= nold && r < rows) {
       *p = to_e4m3(x[i], s, inv);
     } else if (r < nold && grows) {
@@ -194,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void quant_store(QuantStoreLaunch a, int 
       *p = to_e4m3(y, s, inv);
     }
   }
-  if (threadIdx.x == 0) *scale = s;
+  if (on && tt == 0) *scale = s;
   if (!is_k || !a.k_min) return;
 
   float mn[8], mx[8];
@@ -203,62 +244,67 @@ __global__ __launch_bounds__(kThreads) void quant_store(QuantStoreLaunch a, int 
     mn[e] = INFINITY;
     mx[e] = -INFINITY;
   }
+  if (on)
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int r = (threadIdx.x + i * kThreads) / C;
-    if (r < nold || r >= rows) continue;
+    for (int i = 0; i < VPT; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      mn[e] = fminf(mn[e], x[i][e]);
-      mx[e] = fmaxf(mx[e], x[i][e]);
-    }
-  }
-  float lo, hi;
-  reduce_bounds<D>(mn, mx, s_red, &lo, &hi);
-  if (threadIdx.x < D) {
-    const int64_t at = (int64_t)(k.row >> a.block_shift) * D + threadIdx.x;
-    T* pmin = (T*)a.k_min + at;
-    T* pmax = (T*)a.k_max + at;
+      for (int e = 0; e < 8; ++e) {
+        mn[e] = fminf(mn[e], x[i][e]);
+        mx[e] = fmaxf(mx[e], x[i][e]);
+      }
+  team_bounds<D, W>(mn, mx, s_red);
+  if (on && tt < C) {
+    const int64_t at = (int64_t)(k.row >> a.block_shift) * D + tt * 8;
     if (nold > 0) {
-      lo = fminf(lo, (float)*pmin);
-      hi = fmaxf(hi, (float)*pmax);
+      float lo[8], hi[8];
+      load8((const T*)a.k_min + at, lo);
+      load8((const T*)a.k_max + at, hi);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        mn[e] = fminf(mn[e], lo[e]);
+        mx[e] = fmaxf(mx[e], hi[e]);
+      }
     }
-    *pmin = (T)lo;
-    *pmax = (T)hi;
+    store8((T*)a.k_min + at, mn);
+    store8((T*)a.k_max + at, mx);
   }
 }
 
-// One workgroup per (kv head, block).
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void block_bounds(BlockBoundsLaunch a, int nblk) {
-  constexpr int C = D / 8, RPI = kThreads / C;
-  __shared__ float s_red[2 * (kThreads / 64) * D];
-  const int u = blockIdx.x / nblk;
+// Bounds of whole blocks from a bf16 or fp32 cache, teams as above.
+template <typename T, int D, int W, int VPT>
+__global__ __launch_bounds__(kThreads) void block_bounds(BlockBoundsLaunch a, int nblk, int blocks) {
+  constexpr int C = D / 8;
+  __shared__ float s_red[W > 1 ? 2 * (kThreads / 64) * D : 1];
+  const int team = blockIdx.x * (kThreads / 64 / W) + (threadIdx.x >> 6) / W, tt = threadIdx.x & (64 * W - 1);
+  const int u = team / nblk;
   Block k;
-  if (!find_block(a.kv, a.tok, a.block_shift, u, blockIdx.x - u * nblk, &k)) return;
-  const int rows = k.hi - k.at;
-  const T* src = (const T*)a.kv.k + (int64_t)k.row * D + (threadIdx.x % C) * 8;
+  const bool on = team < blocks && find_block(a.kv, a.tok, a.block_shift, u, team - u * nblk, &k);
+  if (W == 1 && !on) return;
   float mn[8], mx[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     mn[e] = INFINITY;
     mx[e] = -INFINITY;
   }
-  for (int r = threadIdx.x / C; r < rows; r += RPI) {
-    float x[8];
-    load8(src + (int64_t)r * D, x);
+  if (on) {
+    const int rows = k.hi - k.at;
+    const T* src = (const T*)a.kv.k + (int64_t)k.row * D + (tt % C) * 8;
+    float x[VPT][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      mn[e] = fminf(mn[e], x[e]);
-      mx[e] = fmaxf(mx[e], x[e]);
-    }
+    for (int i = 0; i < VPT; ++i) load8(src + (int64_t)min((tt + i * 64 * W) / C, rows - 1) * D, x[i]);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        mn[e] = fminf(mn[e], x[i][e]);
+        mx[e] = fmaxf(mx[e], x[i][e]);
+      }
   }
-  float lo, hi;
-  reduce_bounds<D>(mn, mx, s_red, &lo, &hi);
-  if (threadIdx.x < D) {
-    const int64_t at = (int64_t)(k.row >> a.block_shift) * D + threadIdx.x;
-    ((T*)a.k_min)[at] = (T)lo;
-    ((T*)a.k_max)[at] = (T)hi;
+  team_bounds<D, W>(mn, mx, s_red);
+  if (on && tt < C) {
+    const int64_t at = (int64_t)(k.row >> a.block_shift) * D + tt * 8;
+    store8((T*)a.k_min + at, mn);
+    store8((T*)a.k_max + at, mx);
   }
 }
 
@@ -271,16 +317,46 @@ int touched_blocks(const KvView& kv, const NewTokens& tok, int shift) {
   return any < all ? any : all;
 }
 
+// f(W, VPT) as compile-time numbers: waves per block, up to four, and vectors of 8
+// elements per thread.
+template <int N>
+struct Const {
+  static constexpr int value = N;
+};
+template <int D, typename F>
+void with_team(int shift, F f) {
+  switch (shift) {
+    case 4:
+      if constexpr (D == 64) f(Const<1>(), Const<2>());
+      else f(Const<1>(), Const<4>());
+      break;
+    case 5: f(Const<D / 64>(), Const<4>()); break;
+    case 6: f(Const<D / 32>(), Const<4>()); break;
+    default:
+      if constexpr (D == 64) f(Const<4>(), Const<4>());
+      else f(Const<4>(), Const<8>());
+  }
+}
+
 template <typename T, int D>
 hipError_t launch_store_typed(const QuantStoreLaunch& a, int nblk, hipStream_t stream) {
-  const dim3 grid(a.kv.batch * a.kv.hkv * nblk, 2);
-  switch ((D << a.block_shift) / (8 * kThreads)) {
-    case 0:
-    case 1: hipLaunchKernelGGL((quant_store<T, D, 1>), grid, dim3(kThreads), 0, stream, a, nblk); break;
-    case 2: hipLaunchKernelGGL((quant_store<T, D, 2>), grid, dim3(kThreads), 0, stream, a, nblk); break;
-    case 4: hipLaunchKernelGGL((quant_store<T, D, 4>), grid, dim3(kThreads), 0, stream, a, nblk); break;
-    default: hipLaunchKernelGGL((quant_store<T, D, 8>), grid, dim3(kThreads), 0, stream, a, nblk); break;
-  }
+  const int blocks = a.kv.batch * a.kv.hkv * nblk;
+  with_team<D>(a.block_shift, [&](auto w, auto v) {
+    constexpr int W = decltype(w)::value, V = decltype(v)::value, per = kThreads / 64 / W;
+    hipLaunchKernelGGL((quant_store<T, D, W, V>), dim3((blocks + per - 1) / per, 2), dim3(kThreads), 0,
+                       stream, a, nblk, blocks);
+  });
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_bounds_typed(const BlockBoundsLaunch& a, int nblk, hipStream_t stream) {
+  const int blocks = a.kv.batch * a.kv.hkv * nblk;
+  with_team<D>(a.block_shift, [&](auto w, auto v) {
+    constexpr int W = decltype(w)::value, V = decltype(v)::value, per = kThreads / 64 / W;
+    hipLaunchKernelGGL((block_bounds<T, D, W, V>), dim3((blocks + per - 1) / per), dim3(kThreads), 0,
+                       stream, a, nblk, blocks);
+  });
   return hipGetLastError();
 }
 
@@ -299,15 +375,11 @@ hipError_t launch_quant_store(const QuantStoreLaunch& a, hipStream_t stream) {
 hipError_t launch_block_bounds(const BlockBoundsLaunch& a, hipStream_t stream) {
   const int nblk = touched_blocks(a.kv, a.tok, a.block_shift);
   if (nblk == 0) return hipSuccess;
-  const dim3 grid(a.kv.batch * a.kv.hkv * nblk), block(kThreads);
-  if (a.dtype == 1) {
-    if (a.kv.d == 128) hipLaunchKernelGGL((block_bounds<__bf16, 128>), grid, block, 0, stream, a, nblk);
-    else hipLaunchKernelGGL((block_bounds<__bf16, 64>), grid, block, 0, stream, a, nblk);
-  } else {
-    if (a.kv.d == 128) hipLaunchKernelGGL((block_bounds<float, 128>), grid, block, 0, stream, a, nblk);
-    else hipLaunchKernelGGL((block_bounds<float, 64>), grid, block, 0, stream, a, nblk);
-  }
-  return hipGetLastError();
+  if (a.dtype == 1)
+    return a.kv.d == 128 ? launch_bounds_typed<__bf16, 128>(a, nblk, stream)
+                         : launch_bounds_typed<__bf16, 64>(a, nblk, stream);
+  return a.kv.d == 128 ? launch_bounds_typed<float, 128>(a, nblk, stream)
+                       : launch_bounds_typed<float, 64>(a, nblk, stream);
 }
 
 }  // namespace prhs

@@ -161,20 +161,6 @@ __device__ __forceinline__ f16x8_t f16_of_e4m3(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(f16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
-// Maximum over all 64 lanes of non-negative numbers' bits, in every lane.
-__device__ __forceinline__ int wave_imax(int v) {
-#define PRHS_ROR_IMAX(CTRL) v = max(v, __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false))
-  PRHS_ROR_IMAX(0x128);
-  PRHS_ROR_IMAX(0x124);
-  PRHS_ROR_IMAX(0x122);
-  PRHS_ROR_IMAX(0x121);
-#undef PRHS_ROR_IMAX
-  const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-  v = max((int)a[0], (int)a[1]);
-  const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
-  return max((int)b[0], (int)b[1]);
-}
-
 // Lane (col, grp) owns query head col (with !WIDE col mod 8) and in the V product
 // the rows 16 s + 4 grp + e of the tile, in the order 4 s + e.
 template <int D, int QP, bool WIDE>
@@ -380,7 +366,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
     int g1 = rows.page(p1);
     for (int i = 0; i < iters; ++i) {
       const uint32_t ok = T.ok;
-      const int ve = max(wave_imax(__float_as_int((ok >> (lane & (kTile - 1))) & 1u ? T.vs : 0.f)) >> 23, 1);
+      const uint32_t vs = (ok >> (lane & (kTile - 1))) & 1u ? __float_as_uint(T.vs) & 0x7FFFFFFFu : 0u;
+      const int ve = max((int)(wave_umax(vs) >> 23), 1);
       __builtin_amdgcn_wave_barrier();
       stage_tile<D>(T, a.scale_log2, s_k, s_v, s_sc, lane);
       __builtin_amdgcn_wave_barrier();
