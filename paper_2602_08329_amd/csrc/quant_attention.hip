@@ -39,6 +39,7 @@ typedef uint32_t u32x4_a2_t __attribute__((ext_vector_type(4), aligned(2)));
 
 struct QuantArgs : AttnArgs {
   QuantScales sc;
+  int by_length;   // workgroups take their units longest sequence first
 };
 
 constexpr int kTile = 32;   // rows of a wave's tile
@@ -285,7 +286,10 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
   // dynamic LDS: per-wave regions, then the query operands of fp32 queries
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
   __shared__ float sm_m[kMaxWaves][16], sm_l[kMaxWaves][16];
-  const int split = blockIdx.x % a.nsplit, u = blockIdx.x / a.nsplit;
+  __shared__ int s_unit;
+  const int split = blockIdx.x % a.nsplit;
+  int u = blockIdx.x / a.nsplit;
+  if (DENSE && a.by_length) u = unit_of_length_rank(a.kv, a.kv.hkv, u, (int*)dyn, &s_unit);
   const int hkv = a.kv.hkv, hq = a.kv.hq, G = hq / hkv;
   const int wbytes = wave_bytes(D, G);
   const int nwaves = blockDim.x >> 6;
@@ -477,9 +481,12 @@ int waves_for(long long groups, int chunk) {
 }
 
 template <int D, bool DENSE, bool PAGED, int QP, bool WIDE>
-hipError_t launch_typed(const QuantArgs& a, hipStream_t stream) {
+hipError_t launch_typed(QuantArgs& a, hipStream_t stream) {
   const int units = a.kv.batch * a.kv.hkv, G = a.kv.hq / a.kv.hkv;
   const int waves = waves_for((long long)units * a.nsplit, a.chunk);
+  // long whole streams on more units than CUs, which take another as they end
+  // (64 ragged sequences of 8k to 16k, 8 kv heads: 258 us in index order, 242)
+  a.by_length = DENSE && a.nsplit == 1 && units > kCus && a.chunk > 8192 && a.kv.batch > 1 && a.kv.batch <= 1024;
   const size_t dyn = (size_t)waves * wave_bytes(D, G) + query_bytes(D, QP);
   if (dyn > 49152) {
     const hipError_t e = hipFuncSetAttribute((const void*)quant_attn_split<D, DENSE, PAGED, QP, WIDE>,
@@ -496,7 +503,7 @@ hipError_t launch_typed(const QuantArgs& a, hipStream_t stream) {
 }
 
 template <int D, bool DENSE, bool PAGED>
-hipError_t launch_query(const QuantArgs& a, int dtype, hipStream_t stream) {
+hipError_t launch_query(QuantArgs& a, int dtype, hipStream_t stream) {
   if (a.kv.hq / a.kv.hkv > 8)
     return dtype == 1 ? launch_typed<D, DENSE, PAGED, 1, true>(a, stream)
                       : launch_typed<D, DENSE, PAGED, 3, true>(a, stream);
@@ -505,7 +512,7 @@ hipError_t launch_query(const QuantArgs& a, int dtype, hipStream_t stream) {
 }
 
 template <int D, bool DENSE>
-hipError_t launch_layout(const QuantArgs& a, int dtype, hipStream_t stream) {
+hipError_t launch_layout(QuantArgs& a, int dtype, hipStream_t stream) {
   return a.kv.paged ? launch_query<D, DENSE, true>(a, dtype, stream)
                     : launch_query<D, DENSE, false>(a, dtype, stream);
 }

@@ -168,6 +168,14 @@ def test_dense_splits(lens, hq, hkv, d, paged, dtype):
     c.check(*dense(c), lambda b, g: range(lens[b]), some)
 
 
+@pytest.mark.parametrize("paged", [False, True])
+def test_dense_long_streams_of_many_units(paged):
+    # more units than CUs, streams that are not split: longest first, eight waves
+    lens = tuple(8300 if b == 97 else 5000 if b == 3 else 0 if b == 40 else 1 + b % 50 for b in range(260))
+    c = Cache(lens, 2, 1, 64, 16, paged, "bf16", seed=12)
+    c.check(*dense(c), lambda b, g: range(lens[b]))
+
+
 @pytest.mark.parametrize("spread", [0.0, 10.0])
 def test_scales_far_apart(spread):
     # block scales of V over a factor of 2^20: weights of the smaller blocks keep
