@@ -370,3 +370,123 @@ class GatedDecodeRunner(DecodeRunner):
     def retrieving_units(self):
         """Units of every group that retrieved at the last gated step."""
         return int((self.choice < 0).sum().item())
+
+
+class QuantDecodeRunner:
+    """The decode schedule over an 8-bit cache, with whole blocks selected by
+    their key bounds: the prompts of a synthetic workload are stored at once
+    (prhs_quant_store); decode step j stores its token in every layer, the
+    anchor layer of each group selects blocks at j mod s == 0
+    (prhs_block_select), and every layer attends that set plus the tokens since
+    (prhs_quant_reuse_decode_attn).  Blocks are the cache's pages, or
+    block_size tokens of a contiguous cache.
+
+    State: per layer the cache, its scales and its key bounds; per group the
+    chosen blocks and their set; the anchor lengths are the lengths of the
+    refresh step."""
+
+    def __init__(self, inp, device="cuda", block_size=16):
+        w = self.w = inp.w
+        self.inp = inp
+        dev = self.device = torch.device(device)
+        self.L = len(inp.K)
+        self.groups = (self.L + w.G - 1) // w.G
+        self.scale = 1.0 / math.sqrt(w.d)
+        T, Bsz, H, d, i32 = w.steps, w.batch, w.hkv, w.d, torch.int32
+        dt = inp.q.dtype
+        lens = torch.tensor([[n + j + 1 for n in w.n_ctx] for j in range(T)], dtype=i32)
+        self.seq_lens = lens.to(dev)
+        self.max_seq_len = w.capacity
+        self.params = B.params(k=w.k, k_num=w.k_num, k_den=w.k_den, sink=w.sink, window=w.window,
+                               refresh_every=w.s, layer_group=w.G)
+        table = inp.block_table.to(dev) if inp.block_table is not None else None
+        if table is not None:
+            bs, shape = w.page_size, (inp.num_pages, H, w.page_size, d)
+            per_block = (inp.num_pages, H)
+        else:
+            bs, nb = block_size, -(-w.capacity // block_size)
+            shape, per_block = (Bsz, H, nb * bs, d), (Bsz, H, nb)
+        self.block_size = bs
+        n_ctx = torch.tensor(w.n_ctx, dtype=i32, device=dev)
+        self.kv, self.bounds, self.tokens = [], [], []
+        for l in range(self.L):
+            K, V = self._in_order(inp.K[l], table), self._in_order(inp.V[l], table)
+            kv = B.QuantKV(*(torch.zeros(shape, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+                             for _ in "kv"),
+                           *(torch.ones(per_block, dtype=torch.float32, device=dev) for _ in "kv"),
+                           n_ctx, self.max_seq_len, w.hq, table, dtype=dt)
+            bounds = B.BlockBounds(kv, *(torch.zeros(*per_block, d, dtype=dt, device=dev) for _ in "kv"))
+            n = max(w.n_ctx)
+            if n:
+                B.prhs_quant_store(kv, K[:, :, :n].contiguous(), V[:, :, :n].contiguous(), n_ctx, bounds)
+            # the steps' tokens, [T] of [B][Hkv][1][d]
+            at = (self.seq_lens.long() - 1)[:, :, None, None, None].expand(T, Bsz, H, 1, d)
+            self.tokens.append([X.expand(T, *X.shape).gather(3, at).unbind(0) for X in (K, V)])
+            self.kv.append([kv.with_seq_lens(self.seq_lens[j]) for j in range(T)])
+            self.bounds.append(bounds)
+        kv0, G_ = self.kv[0][0], self.groups
+        self.blk_cap = max(1, B.prhs_max_blocks(self.params, bs, self.max_seq_len))
+        self.set_cap = max(1, B.prhs_block_set_capacity(self.params, bs, self.max_seq_len))
+
+        def zeros(*s, dtype=i32):
+            return torch.zeros(*s, dtype=dtype, device=dev)
+
+        self.blocks = [(zeros(Bsz, H, self.blk_cap), zeros(Bsz, H)) for _ in range(G_)]
+        self.sets = [(zeros(Bsz, H, self.set_cap), zeros(Bsz, H)) for _ in range(G_)]
+        self.anchor_step = [None] * G_
+        self.ws_select = B.workspace(B.prhs_block_workspace_size(kv0, self.bounds[0]), dev)
+        self.ws_attn = B.workspace(B.prhs_workspace_size(B.PRHS_OP_QUANT_SPARSE_ATTN, kv0, None, self.set_cap), dev)
+        self.ws_dense = B.workspace(B.prhs_workspace_size(B.PRHS_OP_QUANT_DENSE_ATTN, kv0), dev)
+        self.out = zeros(Bsz, w.hq, d, dtype=torch.float32)
+        self.lse = zeros(Bsz, w.hq, dtype=torch.float32)
+
+    def _in_order(self, X, table):
+        """A layer's keys or values as [B][Hkv][tokens][d]."""
+        if table is None:
+            return X
+        P = X[table.long()]                                  # [B][pages][Hkv][ps][d]
+        return P.permute(0, 2, 1, 3, 4).reshape(P.shape[0], P.shape[2], -1, P.shape[4])
+
+    def store(self, l, j):
+        k, v = self.tokens[l]
+        B.prhs_quant_store(self.kv[l][j], k[j], v[j], None, self.bounds[l])
+
+    def refresh(self, gi, j):
+        l = gi * self.w.G
+        B.prhs_block_select(self.kv[l][j], self.inp.q[l, j], self.params, self.bounds[l],
+                            *self.blocks[gi], *self.sets[gi], self.ws_select)
+        self.anchor_step[gi] = j
+
+    def attend(self, l, j, out=None, lse=None):
+        gi = l // self.w.G
+        j0 = self.anchor_step[gi]
+        if j0 is None or j - j0 >= self.w.s or j < j0:
+            raise RuntimeError(f"group {gi} has no anchor for step {j}")
+        B.prhs_quant_reuse_decode_attn(self.kv[l][j], self.inp.q[l, j], *self.sets[gi],
+                                       self.seq_lens[j0], self.scale,
+                                       self.out if out is None else out,
+                                       self.lse if lse is None else lse, self.ws_attn)
+
+    def dense(self, l, j, out=None, lse=None):
+        B.prhs_quant_dense_decode_attn(self.kv[l][j], self.inp.q[l, j], self.scale,
+                                       self.out if out is None else out,
+                                       self.lse if lse is None else lse, self.ws_dense)
+
+    def step(self, j, outs=None):
+        """One decode step j over every layer: the token's store, the refresh of
+        the groups that it is due for, and attention; outs[l] receives layer l's
+        (out, lse) when given."""
+        for l in range(self.L):
+            self.store(l, j)
+        if B.prhs_schedule(j, 0, self.params) == B.PRHS_REFRESH:
+            for gi in range(self.groups):
+                self.refresh(gi, j)
+        for l in range(self.L):
+            o = None if outs is None else outs[l]
+            self.attend(l, j, *(o if o is not None else (None, None)))
+
+    def dense_step(self, j, outs=None):
+        """Dense attention of step j over every layer, whose tokens are stored."""
+        for l in range(self.L):
+            o = None if outs is None else outs[l]
+            self.dense(l, j, *(o if o is not None else (None, None)))

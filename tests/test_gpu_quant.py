@@ -1,12 +1,5 @@
 """The 8-bit KV cache on the GPU against its fp64 oracle: the store, attention
-over the cache, key bounds and the selection of blocks.
-
-Attention tolerance.  With u = 2^-24, a logit x = scale sum_d q_d k_d is off by
-at most dx = (d + 8) u scale sum_d |q_d k_d| + 4 u |x| (fp32 products and sums,
-scale factors, the exponent's argument), a weight by dx and 2^-21 relative (the
-exponential, its fp16 pair), and fp32 sums of at most n / 32 + 64 terms by as
-many u.  y is off by at most twice the weights' relative error times max |v|,
-lse by the weights' relative error and 4 u |lse|."""
+over the cache, key bounds and the selection of blocks."""
 
 import math
 
@@ -17,6 +10,7 @@ import torch
 import oracle as O
 from oracle import quant_oracle as Q
 from paper_2602_08329_amd import binding as B
+from tests.quant_tolerance import assert_attention
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -101,7 +95,7 @@ class Cache:
         assert (self.ws_all[-256:] == 255).all()
         y, lse = y.double().cpu().numpy(), lse.double().cpu().numpy()
         q = self.q.double().cpu().numpy()
-        G, u = self.hq // self.hkv, 2.0 ** -24
+        G = self.hq // self.hkv
         for b in range(len(self.lens)):
             for g in range(self.hkv):
                 if some is not None and (b, g) not in some:
@@ -113,12 +107,7 @@ class Cache:
                         assert (y[b, h] == 0).all() and lse[b, h] == -math.inf
                         continue
                     yr, lr = O.dense_attention(q[b, h], K, V, self.scale_q)
-                    x = np.abs(K @ q[b, h]) * self.scale_q
-                    dx = ((self.d + 8) * u * self.scale_q * (np.abs(K) @ np.abs(q[b, h]))).max() + 4 * u * x.max()
-                    rel = dx + 2.0 ** -21 + (len(S) / 32 + 64) * u
-                    top = np.abs(V).max()
-                    assert np.abs(y[b, h] - yr).max() <= 2 * rel * top, (b, h, np.abs(y[b, h] - yr).max(), 2 * rel * top)
-                    assert abs(lse[b, h] - lr) <= rel + 4 * u * abs(lr), (b, h, lse[b, h], lr)
+                    assert_attention(y[b, h], lse[b, h], yr, lr, q[b, h], K, V, self.scale_q, (b, h))
 
 
 def dense(c):
@@ -690,3 +679,83 @@ def test_graph_replays_equal_the_eager_calls():
             va, vb = (t.view(torch.uint8) if t.dtype == E4 else t for t in (a, b))
             assert torch.equal(torch.nan_to_num(va.float()), torch.nan_to_num(vb.float()))
         torch.randn(1000, device=DEV).sum().item()   # eager work between the replays
+
+
+def every_call(monkeypatch=None):
+    """Outputs of one call of every entry point of the 8-bit cache and the blocks."""
+    res = []
+
+    def keep(*shape, dtype=I32):
+        res.append(torch.zeros(*shape, dtype=dtype, device=DEV))
+        return res[-1]
+
+    lens, hq, hkv, d = (300, 77), 8, 2, 64
+    c = Cache(lens, hq, hkv, d, 16, True, "bf16", seed=40)
+    lo = torch.randn(c.pages, hkv, d, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).bfloat16()
+    hi = lo + 1
+    bounds = B.BlockBounds(c.kv, lo, hi)
+    new = torch.ones(2, hkv, 3, d, dtype=torch.bfloat16, device=DEV)
+    B.prhs_quant_store(c.kv, new, new, torch.tensor([2, 3], dtype=I32, device=DEV), bounds)
+    B.prhs_quant_store(c.kv, new, new)
+    p = B.params(k=40, sink=4, window=8)
+    kc, sc = B.prhs_max_blocks(p, 16, 300), B.prhs_block_set_capacity(p, 16, 300)
+    blk, bl, st, sl = keep(2, hkv, kc), keep(2, hkv), keep(2, hkv, sc), keep(2, hkv)
+    B.prhs_block_select(c.kv, c.q, p, bounds, blk, bl, st, sl, B.workspace(B.prhs_block_workspace_size(c.kv, bounds), DEV))
+    ws = B.workspace(max(B.prhs_workspace_size(B.PRHS_OP_QUANT_SPARSE_ATTN, c.kv, None, sc),
+                         B.prhs_workspace_size(B.PRHS_OP_QUANT_DENSE_ATTN, c.kv)), DEV)
+    f32 = dict(dtype=torch.float32)
+    ids, tail = torch.arange(4, dtype=I32, device=DEV), c.seq.repeat_interleave(2).contiguous()
+    out = lambda: (keep(2, hq, d, **f32), keep(2, hq, **f32))  # noqa: E731
+    B.prhs_quant_dense_decode_attn(c.kv, c.q, c.scale_q, *out(), ws)
+    B.prhs_quant_sparse_decode_attn(c.kv, c.q, st, sl, c.scale_q, *out(), ws)
+    B.prhs_quant_reuse_decode_attn(c.kv, c.q, st, sl, c.seq, c.scale_q, *out(), ws)
+    B.prhs_quant_pool_decode_attn(c.kv, c.q, st, sl, ids, tail, c.scale_q, *out(), ws, psaw=B.psaw(3, 4, 1, 0.5, 1.0, 4))
+    K = torch.randn(2, hkv, 320, d, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).bfloat16()
+    kv = B.KV(K, K, c.seq, 300, hq)
+    bb = B.BlockBounds(kv, keep(2, hkv, 20, d, dtype=torch.bfloat16), keep(2, hkv, 20, d, dtype=torch.bfloat16))
+    B.prhs_block_bounds(kv, bb, 300)
+    B.prhs_block_select(kv, c.q, p, bb, keep(2, hkv, kc), keep(2, hkv), keep(2, hkv, sc), keep(2, hkv),
+                        B.workspace(B.prhs_block_workspace_size(kv, bb), DEV))
+    torch.cuda.synchronize()
+    return res + [c.dev["k"].view(torch.uint8), c.dev["v"].view(torch.uint8), lo, hi]
+
+
+def test_native_marshalling_equals_python(monkeypatch):
+    if B._host is None:
+        pytest.skip("the extension is not built")
+    host, taken = B._host, []
+
+    class Watch:
+        def __getattr__(self, name):
+            def f(*a):
+                r = getattr(host, name)(*a)
+                if r is not None:
+                    taken.append(name)
+                return r
+            return f
+
+    monkeypatch.setattr(B, "_host", Watch())
+    native = every_call()
+    assert set(taken) == {"quant_store", "quant_dense", "quant_sparse", "quant_reuse", "quant_pool", "block_bounds", "block_select"}
+    assert taken.count("block_select") == 2 and taken.count("quant_store") == 2
+    monkeypatch.setattr(B, "_host", None)
+    for x, y in zip(native, every_call()):
+        assert torch.equal(x, y)
+
+
+def test_what_does_not_fit_raises_from_the_native_path_too():
+    c = Cache((300, 77), 8, 2, 64, 16, True, "bf16", seed=41)
+    y, lse = c.outputs()
+    ws = c.workspace(True)
+    new = torch.ones(2, 2, 3, 64, dtype=torch.bfloat16, device=DEV)
+    for bad in (lambda: B.prhs_quant_dense_decode_attn(c.kv, c.q.float(), 1.0, y, lse, ws),
+                lambda: B.prhs_quant_dense_decode_attn(c.kv, c.q.cpu(), 1.0, y, lse, ws),
+                lambda: B.prhs_quant_dense_decode_attn(c.kv, c.q, 1.0, y[:1], lse, ws),
+                lambda: B.prhs_quant_store(c.kv, new, new[:, :1].contiguous()),
+                lambda: B.prhs_quant_store(c.kv, new, new, torch.zeros(3, dtype=I32, device=DEV))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(B.PrhsError) as e:
+        B.prhs_quant_dense_decode_attn(c.kv, c.q, 1.0, y, lse, ws[:16])
+    assert e.value.status == B.PRHS_E_WORKSPACE
+    assert (y == 7).all()
