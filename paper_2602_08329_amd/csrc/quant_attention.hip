@@ -316,7 +316,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
     rows.idx = a.set_idx + (size_t)row * a.set_cap;
     rows.set_last = max(a.set_cap, 1) - 1;
   }
-  const bool any = DENSE || a.set_cap > 0;
+  const bool any = DENSE || (a.set_cap > 0 && (!a.unit_row || a.pool_rows > 0));
   int raw0 = any ? rows.entry(t) : -1, raw1 = any ? rows.entry(t + step) : -1,
       raw2 = any ? rows.entry(t + 2 * step) : -1;
   // a dense stream's first tile loads before the lengths are known: its positions

@@ -256,6 +256,27 @@ def test_pool_rows_sides_and_window():
         c.check(y, lse, lambda b, g: want(b, g, window))
 
 
+def test_empty_pool_and_empty_sets():
+    # no row of the pool, no entry of a set: every output is that of no tokens
+    import ctypes
+    c = Cache((60, 40), 4, 2, 64, 16, True, "bf16", seed=7)
+    i = torch.zeros(4, 8, dtype=I32, device=DEV)
+    tail = torch.full((4,), 100, dtype=I32, device=DEV)
+    ptr = [ctypes.c_void_p(t.data_ptr()) for t in (c.q, i, tail, i, tail)]
+    for call in ("pool", "sparse"):
+        y, lse = c.outputs()
+        ws = c.workspace(False, 8)
+        o = [ctypes.c_void_p(t.data_ptr()) for t in (y, lse, ws)]
+        L, st = B.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        if call == "pool":
+            B.check(L.prhs_quant_pool_decode_attn(ctypes.byref(c.kv.quant), ptr[0], ptr[1], ptr[2], 0, 8, ptr[3], ptr[4],
+                                                  None, 0, None, 0.1, *o, ws.numel(), st))
+        else:
+            B.check(L.prhs_quant_sparse_decode_attn(ctypes.byref(c.kv.quant), ptr[0], ptr[1], ptr[2], 0, 0.1, *o,
+                                                    ws.numel(), st))
+        assert (y == 0).all() and (lse == -math.inf).all()
+
+
 def test_pages_outside_the_pool_and_lengths_beyond_the_bound():
     lens = (100, 64)
     c = Cache(lens, 4, 2, 128, 16, True, "bf16", seed=8)
