@@ -6,7 +6,7 @@
 // bounds (4d bytes a block in bf16) once: 512 rows of 4096 blocks at d 128 (1.07
 // GB) 181 us, 5.9 TB/s, where a kernel that only loads them in the same order
 // takes 150.  The scoring without its arithmetic takes the same time; the pick
-// costs a row of 8192 blocks 9 us in a launch of its own.
+// costs a row of 8192 blocks 8 us in a launch of its own.
 //
 // Scores become order-preserving keys (0, below every number's key, for NaN and
 // for blocks whose page lies outside the pool).  The key of the last chosen block
@@ -30,14 +30,14 @@ constexpr int kThreads = 512;        // scoring workgroups, and select_blocks
 constexpr int kWaves = kThreads / 64;
 constexpr int kPickThreads = 1024;
 constexpr int kBins = 2048;
+constexpr int kKeys = 8;             // most keys a thread of the pick holds at a time
 constexpr int kRankMax = 64;         // candidates for the last key that one wave ranks
 constexpr int kListMax = 4096;       // chosen blocks kept in LDS
 constexpr int kLdsKeys = 14336;      // most keys a workgroup holds in LDS (56 KB)
 
 struct BlockArgs : BlockSelectLaunch {
   uint32_t* keys;   // [units][nbmax], candidate i of a unit at [i]
-  int nbmax;
-  int lds_keys;     // select_blocks: keys in LDS, at least nbmax
+  int nbmax;        // blocks of the longest row, a multiple of kKeys
   int lds_list;     // chosen blocks in LDS
   int chunk;        // score_blocks: candidates of a workgroup
 };
@@ -300,33 +300,39 @@ struct PickLds {
   uint32_t ncand, bin, left, count, key;
 };
 
-// A wave's share of a row's n keys, in order: rounds of 64, key 64 j + lane of
-// round j.  With R > 0 rounds they are in registers, else read from `keys`.
+// A row's n keys over a workgroup of NT threads, R consecutive ones a thread (so
+// that a scan over the threads is in block order), in chunks of NT R: one chunk
+// stays in registers, more are read again by each pass.
+// `keys` holds a multiple of R.
 template <int NT, int R>
-struct WaveKeys {
-  uint32_t x[R > 0 ? R : 1];
+struct RowKeys {
+  typedef uint32_t vec_t __attribute__((ext_vector_type(R), aligned(4)));
+  uint32_t x[R];
   const uint32_t* keys;
-  int n, begin, rounds;
+  int room, n;
 
-  __device__ __forceinline__ void init(const uint32_t* from, int count) {
-    keys = from;
-    n = count;
-    rounds = R > 0 ? R : (n + NT - 1) / NT;
-    begin = (int)(threadIdx.x >> 6) * rounds * 64 + (int)(threadIdx.x & 63);
+  __device__ __forceinline__ void load(int c) {
+    const int i = (c * NT + (int)threadIdx.x) * R;
+    const vec_t v = *(const vec_t*)(keys + (i < room ? i : 0));
 #pragma unroll
-    for (int j = 0; j < (R > 0 ? R : 0); ++j) x[j] = keys[min(begin + 64 * j, n - 1)];
+    for (int j = 0; j < R; ++j) x[j] = v[j];
   }
-  // f(index, key, whether it is one)
+  __device__ __forceinline__ void init(const uint32_t* from, int padded) {
+    keys = from;
+    room = padded;
+    load(0);
+  }
+  __device__ __forceinline__ int chunks() const { return (n + NT * R - 1) / (NT * R); }
+  // f(key) for each of this thread's keys
   template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-    if constexpr (R > 0) {
+  __device__ __forceinline__ void each(F f) {
+    const int last = chunks();
+    for (int c = 0; c < last; ++c) {
+      if (last > 1) load(c);
+      const int i = (c * NT + (int)threadIdx.x) * R;
 #pragma unroll
-      for (int j = 0; j < R; ++j) f(begin + 64 * j, x[j], begin + 64 * j < n);
-    } else {
-      for (int j = 0; j < rounds; ++j) {
-        const int i = begin + 64 * j;
-        f(i, keys[min(i, n - 1)], i < n);
-      }
+      for (int j = 0; j < R; ++j)
+        if (i + j < n) f(x[j]);
     }
   }
 };
@@ -338,12 +344,12 @@ struct WaveKeys {
 // a rule, where digits of the keys' own bits take two: scores differ little in
 // their exponents.
 template <int NT, typename Keys>
-__device__ uint32_t kth_key(const Keys& keys, uint32_t k, PickLds& s, uint32_t* left) {
+__device__ uint32_t kth_key(Keys& keys, uint32_t k, PickLds& s, uint32_t* left) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t inv = 0u, mx = 0u;   // of the smallest key its complement
-  keys.each([&](int, uint32_t x, bool in) {
-    inv = in ? max(inv, ~x) : inv;
-    mx = in ? max(mx, x) : mx;
+  keys.each([&](uint32_t x) {
+    inv = max(inv, ~x);
+    mx = max(mx, x);
   });
   inv = wave_umax(inv);
   mx = wave_umax(mx);
@@ -364,8 +370,8 @@ __device__ uint32_t kth_key(const Keys& keys, uint32_t k, PickLds& s, uint32_t* 
   for (;;) {
     const int shift = max(0, width - 11);
     const uint32_t span = width >= 32 ? 0xFFFFFFFFu : (1u << width) - 1u;   // largest key - lo
-    keys.each([&](int, uint32_t x, bool in) {
-      if (in && x >= lo && x - lo <= span) atomicAdd(&s.hist[(x - lo) >> shift], 1u);
+    keys.each([&](uint32_t x) {
+      if (x >= lo && x - lo <= span) atomicAdd(&s.hist[(x - lo) >> shift], 1u);
     });
     lds_barrier();
     // the bin of the k-th largest, from the top
@@ -396,8 +402,8 @@ __device__ uint32_t kth_key(const Keys& keys, uint32_t k, PickLds& s, uint32_t* 
     }
     if (count <= (uint32_t)kRankMax) {
       const uint32_t top = (1u << shift) - 1u;
-      keys.each([&](int, uint32_t x, bool in) {
-        if (in && x >= lo && x - lo <= top) s.cand[atomicAdd(&s.ncand, 1u)] = x;
+      keys.each([&](uint32_t x) {
+        if (x >= lo && x - lo <= top) s.cand[atomicAdd(&s.ncand, 1u)] = x;
       });
       lds_barrier();
       // every wave ranks them itself, so that no barrier follows
@@ -423,60 +429,59 @@ __device__ uint32_t kth_key(const Keys& keys, uint32_t k, PickLds& s, uint32_t* 
 // the last candidate are among them.
 template <int NT, int R>
 __device__ __forceinline__ void place_blocks(const BlockArgs& a, const MiddleBlocks& m, int u, int kb,
-                                             const uint32_t* from, int32_t* list, PickLds& s,
+                                             RowKeys<NT, R>& keys, int32_t* list, PickLds& s,
                                              bool* first_in, bool* last_in) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, n = keys.n;
   int32_t* blk = a.blk_idx + (size_t)u * a.blk_cap;
-  WaveKeys<NT, R> keys;
-  keys.init(from, m.count);
-  const uint32_t key0 = from[0], key1 = from[m.count - 1];
+  const uint32_t key0 = keys.keys[0], key1 = keys.keys[n - 1];
   uint32_t left;
   const uint32_t T = kth_key<NT>(keys, (uint32_t)kb, s, &left);
-  uint32_t gt = 0u, eq = 0u;
-  keys.each([&](int, uint32_t x, bool in) {
-    gt += __popcll(__builtin_amdgcn_ballot_w64(in && x > T));
-    eq += __popcll(__builtin_amdgcn_ballot_w64(in && x == T));
-  });
-  if (lane == 0) s.scan[wave] = gt << 16 | eq;   // of a wave, at most 2^14 keys
-  lds_barrier();
-  gt = eq = 0u;
-  uint32_t eq_all = 0u;
+  const int chunks = keys.chunks();
+  uint32_t gt_all = 0u, eq_all = 0u;   // keys above and equal to T in earlier chunks
+  for (int c = 0; c < chunks; ++c) {
+    if (chunks > 1) keys.load(c);
+    const int i = (c * NT + tid) * R;
+    uint32_t is_gt = 0u, is_eq = 0u;   // bit j: key j of this thread
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w) {
-    const uint32_t c = s.scan[w];
-    gt += w < wave ? c >> 16 : 0u;
-    eq += w < wave ? c & 0xFFFFu : 0u;
-    eq_all += c & 0xFFFFu;
-  }
-  *first_in = key0 >= T;   // of equal keys the first ones are chosen
-  *last_in = key1 > T || (key1 == T && eq_all == left);
-  const uint64_t below = ((uint64_t)1 << lane) - 1u;
-  keys.each([&](int i, uint32_t x, bool in) {
-    const uint64_t bg = __builtin_amdgcn_ballot_w64(in && x > T), be = __builtin_amdgcn_ballot_w64(in && x == T);
-    const uint32_t e = eq + __popcll(be & below);
-    if (in && (x > T || (x == T && e < left))) {
-      const uint32_t at = gt + __popcll(bg & below) + min(e, left);
-      blk[at] = m.first + i;
-      if (list) list[at] = m.first + i;
+    for (int j = 0; j < R; ++j) {
+      is_gt |= (i + j < n && keys.x[j] > T ? 1u : 0u) << j;
+      is_eq |= (i + j < n && keys.x[j] == T ? 1u : 0u) << j;
     }
-    gt += __popcll(bg);
-    eq += __popcll(be);
-  });
+    // of a chunk at most 2^13 keys, so that both counts scan in one word
+    const uint32_t mine = (uint32_t)__popc(is_gt) << 16 | (uint32_t)__popc(is_eq);
+    uint32_t total;
+    const uint32_t before = block_exclusive_scan<NT>(mine, s.scan, &total);
+    uint32_t g = gt_all + (before >> 16), e = eq_all + (before & 0xFFFFu);
+    for (uint32_t rest = is_gt | is_eq; rest; rest &= rest - 1u) {
+      const int j = __ffs((int)rest) - 1;
+      const bool above = (is_gt >> j) & 1u;
+      if (above || e < left) {   // of equal keys the first `left`
+        const uint32_t at = g + min(e, left);
+        blk[at] = m.first + i + j;
+        if (list) list[at] = m.first + i + j;
+      }
+      g += above ? 1u : 0u;
+      e += above ? 0u : 1u;
+    }
+    gt_all += total >> 16;
+    eq_all += total & 0xFFFFu;
+  }
+  *first_in = key0 >= T;
+  *last_in = key1 > T || (key1 == T && eq_all == left);
 }
 
 // Writes unit u's chosen blocks and set from its candidates' keys.
-template <int NT>
+template <int NT, int R>
 __device__ __forceinline__ void pick_row(const BlockArgs& a, const MiddleBlocks& m, int u, int kb,
-                                         const uint32_t* keys, int32_t* s_list, PickLds& s) {
+                                         RowKeys<NT, R>& keys, int32_t* s_list, PickLds& s) {
   const int tid = threadIdx.x, n = m.count, bs = 1 << a.block_shift;
   int32_t* blk = a.blk_idx + (size_t)u * a.blk_cap;
   int32_t* set = a.set_idx + (size_t)u * a.set_cap;
   bool first_in = kb > 0, last_in = kb > 0;
   int32_t* list = kb <= a.lds_list ? s_list : nullptr;
   if (kb > 0 && kb < n) {
-    if (n <= 2 * NT) place_blocks<NT, 2>(a, m, u, kb, keys, list, s, &first_in, &last_in);
-    else if (n <= 8 * NT) place_blocks<NT, 8>(a, m, u, kb, keys, list, s, &first_in, &last_in);
-    else place_blocks<NT, 0>(a, m, u, kb, keys, list, s, &first_in, &last_in);
+    keys.n = n;
+    place_blocks<NT, R>(a, m, u, kb, keys, list, s, &first_in, &last_in);
   } else if (kb > 0) {   // every candidate
     for (int i = tid; i < n; i += NT) {
       blk[i] = m.first + i;
@@ -520,17 +525,19 @@ __global__ __launch_bounds__(kThreads) void score_blocks(BlockArgs a, int chunks
   for (int i = begin + threadIdx.x; i < end; i += kThreads) keys[i] = s_keys[i - begin];
 }
 
+template <int R>
 __global__ __launch_bounds__(kPickThreads) void pick_blocks(BlockArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];   // the chosen blocks
   __shared__ PickLds s;
   const int u = blockIdx.x, b = u / a.kv.hkv;
+  RowKeys<kPickThreads, R> keys;   // loaded before the row's length is known
+  keys.init(a.keys + (size_t)u * a.nbmax, a.nbmax);
   const MiddleBlocks m = middle_blocks(a, b);
-  pick_row<kPickThreads>(a, m, u, chosen_blocks(a, m.n0, m.count), a.keys + (size_t)u * a.nbmax,
-                         (int32_t*)dyn, s);
+  pick_row(a, m, u, chosen_blocks(a, m.n0, m.count), keys, (int32_t*)dyn, s);
 }
 
 // LDS: keys, chosen blocks, then the scorer's.
-template <typename T, int D, bool PAGED>
+template <typename T, int D, bool PAGED, int R>
 __global__ __launch_bounds__(kThreads) void select_blocks(BlockArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
   __shared__ PickLds s;
@@ -538,12 +545,14 @@ __global__ __launch_bounds__(kThreads) void select_blocks(BlockArgs a) {
   const MiddleBlocks m = middle_blocks(a, b);
   const int kb = chosen_blocks(a, m.n0, m.count);
   uint32_t* s_keys = (uint32_t*)dyn;
-  int32_t* s_list = (int32_t*)(s_keys + a.lds_keys);
+  int32_t* s_list = (int32_t*)(s_keys + a.nbmax);
   if (kb > 0 && kb < m.count) {
     score_range<T, D, PAGED>(a, m, b, g, 0, m.count, (unsigned char*)(s_list + a.lds_list), s_keys);
     lds_barrier();
   }
-  pick_row<kThreads>(a, m, u, kb, s_keys, s_list, s);
+  RowKeys<kThreads, R> keys;
+  keys.init(s_keys, a.nbmax);
+  pick_row(a, m, u, kb, keys, s_list, s);
 }
 
 // One launch (us, then in two): where a workgroup reads a row in about what the
@@ -570,22 +579,28 @@ hipError_t allow_lds(F* f, size_t bytes) {
   return hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxDynamicLds);
 }
 
+template <int N>
+struct Const {
+  static constexpr int value = N;
+};
+
 template <typename T, int D, bool PAGED>
 hipError_t launch_typed(BlockArgs& a, hipStream_t stream) {
   typedef Scorer<T, D, PAGED> S;
   const int units = a.kv.batch * a.kv.hkv;
   constexpr size_t kScoreLds = S::kLdsQuery + (size_t)kWaves * S::kLdsWave;
-  const int kb = std::min(a.blk_cap, a.nbmax);
-  a.lds_list = (std::min(kb, kListMax) + 3) & ~3;
+  a.lds_list = (std::min(std::min(a.blk_cap, a.nbmax), kListMax) + 3) & ~3;
   const long long row_bytes = (long long)a.nbmax * 2 * D * sizeof(T);
-  const int keys = (a.nbmax + 3) & ~3;
-  if (keys <= kLdsKeys && one_launch(units, row_bytes)) {
-    a.lds_keys = keys;
-    const size_t lds = ((size_t)keys + a.lds_list) * 4 + kScoreLds;
-    const hipError_t e = allow_lds(select_blocks<T, D, PAGED>, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((select_blocks<T, D, PAGED>), dim3(units), dim3(kThreads), lds, stream, a);
-    return hipGetLastError();
+  if (a.nbmax <= kLdsKeys && one_launch(units, row_bytes)) {
+    const size_t lds = ((size_t)a.nbmax + a.lds_list) * 4 + kScoreLds;
+    auto launch = [&](auto r) {
+      constexpr int R = decltype(r)::value;
+      const hipError_t e = allow_lds(select_blocks<T, D, PAGED, R>, lds);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((select_blocks<T, D, PAGED, R>), dim3(units), dim3(kThreads), lds, stream, a);
+      return hipGetLastError();
+    };
+    return a.nbmax <= 2 * kThreads ? launch(Const<2>()) : launch(Const<kKeys>());
   }
   // about four workgroups a CU, of whole rounds of their waves' tiles
   constexpr int round = S::kRows * kWaves;
@@ -599,7 +614,10 @@ hipError_t launch_typed(BlockArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((score_blocks<T, D, PAGED>), dim3((unsigned)units * chunks), dim3(kThreads), lds,
                        stream, a, chunks);
   }
-  hipLaunchKernelGGL(pick_blocks, dim3(units), dim3(kPickThreads), (size_t)a.lds_list * 4, stream, a);
+  if (a.nbmax <= 2 * kPickThreads)
+    hipLaunchKernelGGL(pick_blocks<2>, dim3(units), dim3(kPickThreads), (size_t)a.lds_list * 4, stream, a);
+  else
+    hipLaunchKernelGGL(pick_blocks<kKeys>, dim3(units), dim3(kPickThreads), (size_t)a.lds_list * 4, stream, a);
   return hipGetLastError();
 }
 
@@ -610,15 +628,20 @@ hipError_t launch_layout(BlockArgs& a, hipStream_t stream) {
 
 }  // namespace
 
+// Keys of a row of the workspace.
+static int row_keys(int max_seq_len, int block_shift) {
+  return (((max_seq_len + (1 << block_shift) - 1) >> block_shift) + kKeys - 1) / kKeys * kKeys;
+}
+
 size_t block_select_workspace_bytes(int units, int max_seq_len, int block_shift) {
-  return (size_t)units * ((max_seq_len + (1 << block_shift) - 1) >> block_shift) * sizeof(uint32_t);
+  return (size_t)units * row_keys(max_seq_len, block_shift) * sizeof(uint32_t);
 }
 
 hipError_t launch_block_select(const BlockSelectLaunch& s, hipStream_t stream) {
   BlockArgs a;
   (BlockSelectLaunch&)a = s;
   a.keys = (uint32_t*)s.ws;
-  a.nbmax = (s.kv.max_seq_len + (1 << s.block_shift) - 1) >> s.block_shift;
+  a.nbmax = row_keys(s.kv.max_seq_len, s.block_shift);
   if (s.dtype == 1)
     return s.kv.d == 128 ? launch_layout<__bf16, 128>(a, stream) : launch_layout<__bf16, 64>(a, stream);
   return s.kv.d == 128 ? launch_layout<float, 128>(a, stream) : launch_layout<float, 64>(a, stream);
