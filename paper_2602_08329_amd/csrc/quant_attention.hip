@@ -451,7 +451,7 @@ constexpr long long kCus = 256;
 constexpr int kWholeFew = 768, kWholeMany = 1536, kFewUnits = 64;
 constexpr int kMinSplit = 128;
 constexpr long long kThirdIdle = 176;
-constexpr int kLongRows = 3072;
+constexpr int kLongRows = 4000;
 
 long long splits_of(long long units, long long rows) {
   if (units > kCus) {
