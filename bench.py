@@ -697,7 +697,7 @@ def roofline_of(w, num, copy_traffic=True):
     a = num["attn_launch"]
     achieved = a["avg_bytes"] / (a["avg_us"] * 1e-6) / 1e9
     kern = "attn_split_bf16" if w.dtype != "f32" else "attn_split_f32"
-    traffic = committed_traffic(f"{kern}_{w.name}_pmc.md", "attention.hip")
+    traffic = committed_traffic(f"{kern}_{w.name}_pmc.md", "attention.hip", "attention_common.h")
     return {"kernel": kern + " (sparse)", "bound": "hbm", "achieved": round(achieved, 1),
             "peak": HBM_PEAK_GBPS, "unit": "GB/s", "frac": round(achieved / HBM_PEAK_GBPS, 4),
             "traffic": traffic if copy_traffic else None, "avg_launch_us": round(a["avg_us"], 3),
