@@ -581,7 +581,9 @@ prhs_status prhs_block_workspace_size(const prhs_kv* kv, const prhs_bounds* boun
  * Entries behind the lengths are left as they are.
  * ws: >= prhs_block_workspace_size() bytes, no initialisation needed.
  * NaN scores and blocks on pages outside the pool rank last.  -0.0 ranks
- * equal to +0.0. */
+ * equal to +0.0.  sigma is computed as max(q, 0) . k_max + min(q, 0) . k_min,
+ * the same for finite bounds; an infinite bound that meets a zero there makes
+ * it NaN. */
 prhs_status prhs_block_select(const prhs_kv* kv, const void* q, const prhs_params* params,
                               const prhs_bounds* bounds, int32_t* blk_idx, int32_t* blk_len,
                               int32_t blk_cap, int32_t* set_idx, int32_t* set_len,

@@ -620,6 +620,30 @@ def test_block_select_ties_nan_and_lost_pages(paged):
         check_select(got, lambda b, g: sig[b, g], lens, hkv, lambda m: k, 0, 0, bs)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_block_select_infinite_bounds(dtype):
+    # a score of +inf ranks first, ties to the lower block; where an infinite bound
+    # meets a zero of q's positive or negative part the score is NaN and ranks last
+    n, bs, d, hkv = 700, 32, 128, 2
+    nb = -(-n // bs)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    K = torch.zeros((1, hkv, nb * bs, d), dtype=dt, device=DEV)
+    kv = B.KV(K, K, torch.tensor([n], dtype=I32, device=DEV), n, 4)
+    lo = torch.zeros((1, hkv, nb, d), dtype=dt, device=DEV)
+    hi = lo.clone()
+    hi[:, :, 3, 0] = math.inf    # q > 0
+    lo[:, :, 7, 0] = -math.inf
+    hi[:, :, 9, 1] = math.inf    # q < 0
+    lo[:, :, 11, 1] = -math.inf
+    sig = np.zeros(nb)
+    sig[[3, 11]], sig[[7, 9]] = math.inf, -math.inf
+    q = torch.ones(1, 4, d, dtype=dt, device=DEV)
+    q[:, :, 1] = -1.0
+    for k in (32, 64, 96, bs * (nb - 2), bs * (nb - 1)):
+        got = run_select(kv, B.BlockBounds(kv, lo, hi), q, B.params(k=k, sink=0, window=0), bs, n, hkv, 1)
+        check_select(got, lambda b, g: sig, (n,), hkv, lambda m: k, 0, 0, bs)
+
+
 # ---- together ----------------------------------------------------------------------
 
 def test_store_select_and_attend_as_a_decode_loop():
