@@ -417,9 +417,11 @@ static prhs_status attention_common(const prhs_kv* kv, const prhs::QuantScales* 
   double psaw_f = 0.0;
   if (psaw && (st = psaw_factor(psaw, &psaw_f)) != PRHS_OK) return st;
   const int rows_cap = dense ? kv->max_seq_len : set_cap;
-  if (scales && (st = check_grid(std::max((long long)kv->batch * kv->num_q_heads,
-                                          prhs::quant_attn_groups(kv->batch, kv->num_kv_heads, rows_cap)))) != PRHS_OK)
-    return st;
+  if (scales) {
+    const long long groups = prhs::quant_attn_groups(kv->batch, kv->num_kv_heads, rows_cap);
+    st = check_grid(std::max((long long)kv->batch * kv->num_q_heads, groups));
+    if (st != PRHS_OK) return st;
+  }
   const size_t wsz =
       scales ? prhs::quant_attn_call_bytes(kv->batch, kv->num_q_heads, kv->num_kv_heads,
                                            kv->head_dim, rows_cap)
@@ -498,12 +500,12 @@ prhs_status prhs_reuse_decode_attn(const prhs_kv* kv, const void* q, const int32
                           "prhs_reuse_decode_attn launch");
 }
 
-static prhs_status pool_common(const prhs_kv* kv, const prhs::QuantScales* scales, const void* q, const int32_t* pool_idx,
-                                  const int32_t* pool_len, int32_t pool_rows, int32_t set_cap,
-                                  const int32_t* unit_row, const int32_t* unit_tail,
-                                  const int32_t* unit_gate, int32_t units_side,
-                                  const prhs_psaw* psaw, float scale, float* out, float* lse,
-                                  void* ws, size_t ws_bytes, void* stream,
+static prhs_status pool_common(const prhs_kv* kv, const prhs::QuantScales* scales,
+                               const void* q, const int32_t* pool_idx, const int32_t* pool_len,
+                               int32_t pool_rows, int32_t set_cap, const int32_t* unit_row,
+                               const int32_t* unit_tail, const int32_t* unit_gate,
+                               int32_t units_side, const prhs_psaw* psaw, float scale, float* out,
+                               float* lse, void* ws, size_t ws_bytes, void* stream,
                                const char* name) {
   if (pool_rows < 0) return fail(PRHS_E_INVALID, "pool_rows must be >= 0");
   if (kv && kv->batch > 0 && (!unit_row || !unit_tail))

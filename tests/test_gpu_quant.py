@@ -684,6 +684,50 @@ def test_store_select_and_attend_as_a_decode_loop():
         c.check(y, lse, lambda b, g: sets[b, g] + list(range(n0[b], s.n[b])))
 
 
+@pytest.mark.parametrize("paged", [True, False])
+def test_bytes_behind_four_gigabytes(paged):
+    # the last pages, or the last unit's rows, of a cache that lie behind 2^32 bytes
+    # give what a small cache gives, and nothing else is written
+    batch, hq, hkv, d, bs, n = 2, 8, 4, 128, 64, 700
+    nb = -(-n // bs)
+    big = 2 ** 32 // ((hkv if paged else batch * hkv - 1) * bs * d) + (batch * nb if paged else 1)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    k, v = (torch.randn(batch, hkv, n, d, generator=g, device=DEV).bfloat16() for _ in "kv")
+    q = torch.randn(batch, hq, d, generator=g, device=DEV).bfloat16()
+    seq = torch.tensor([n, n - 70], dtype=I32, device=DEV)
+    p = B.params(k=200, sink=4, window=30)
+    got = []
+    for blocks in (batch * nb, big) if paged else (nb, big):
+        lead = (blocks, hkv) if paged else (batch, hkv, blocks)
+        shape = (blocks, hkv, bs, d) if paged else (batch, hkv, blocks * bs, d)
+        K, V = (torch.zeros(shape, dtype=torch.uint8, device=DEV) for _ in "kv")
+        ks, vs = (torch.ones(lead, device=DEV) for _ in "kv")
+        table = None
+        if paged:
+            table = (blocks - 1 - torch.arange(batch * nb, device=DEV)).view(batch, nb).to(I32)
+        kv = B.QuantKV(K.view(E4), V.view(E4), ks, vs, seq, n, hq, table)
+        lo, hi = (torch.zeros(*lead, d, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+        bounds = B.BlockBounds(kv, lo, hi)
+        B.prhs_quant_store(kv, k, v, None, bounds)
+        sel = run_select(kv, bounds, q, p, bs, n, hkv, batch)
+        outs = []
+        for op in (B.PRHS_OP_QUANT_DENSE_ATTN, B.PRHS_OP_QUANT_SPARSE_ATTN):
+            y, lse = torch.zeros(batch, hq, d, device=DEV), torch.zeros(batch, hq, device=DEV)
+            ws = B.workspace(B.prhs_workspace_size(op, kv, None, sel[2].shape[2]), DEV)
+            if op == B.PRHS_OP_QUANT_DENSE_ATTN:
+                B.prhs_quant_dense_decode_attn(kv, q, 0.1, y, lse, ws)
+            else:
+                B.prhs_quant_sparse_decode_attn(kv, q, sel[2], sel[3], 0.1, y, lse, ws)
+            outs += [y, lse]
+        used = table.flatten().long() if paged else None
+        rows = [x[used] if paged else x[:, :, : nb * bs] for x in (K, V)]
+        outs += [*rows, *(x[used] if paged else x[:, :, :nb] for x in (ks, vs, lo, hi)), *sel]
+        outs += [sum(int(t.count_nonzero()) for t in x.view(-1).split(2 ** 28)) for x in (K, V)]
+        got.append(outs)
+    for i, (a, b) in enumerate(zip(*got)):
+        assert a == b if isinstance(a, int) else torch.equal(a, b), i
+
+
 def test_graph_replays_equal_the_eager_calls():
     batch, hq, hkv, d, bs, n = 3, 8, 2, 64, 16, 3000
     lens = (n, 1200, 65)
