@@ -54,7 +54,7 @@ constexpr int kTile = 32;   // rows of a wave's tile
 // LDS bytes of a wave: its tile of K, of V and their scales, at the end its G
 // output rows.
 __host__ __device__ constexpr int wave_bytes(int D, int G) {
-  const int tile = 2 * kTile * D + 2 * kTile * 4, out = G * (D + 1) * 4;
+  const int tile = 2 * kTile * D + 2 * kTile * 4, out = G * (D + 4) * 4;
   return ((tile > out ? tile : out) + 15) & ~15;
 }
 
@@ -406,35 +406,41 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
   }
   const float unscale = st.r > 0.f ? 1.f / st.r : 0.f;
   __builtin_amdgcn_wave_barrier();
-  float* wo = (float*)own + col * (D + 1);
+  float* wo = (float*)own + col * (D + 4) + 4 * grp;
 #pragma unroll
-  for (int blk = 0; blk < D / 16; ++blk)
+  for (int blk = 0; blk < D / 16; ++blk) {
+    f32x4_t v = st.o[blk] * unscale;
+    if (!WIDE)   // hi and lo: columns 8 apart
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float v = st.o[blk][i] * unscale;
-      if (!WIDE) v = add_rotated<0x128>(v);   // hi and lo: columns 8 apart
-      if (col < G) wo[16 * blk + 4 * grp + i] = v;
-    }
+      for (int i = 0; i < 4; ++i) v[i] = add_rotated<0x128>(v[i]);
+    if (col < G) *(f32x4_t*)(wo + 16 * blk) = v;
+  }
   __syncthreads();
+  // four dims a thread and step, the waves' rows read four at a time
   const int nsp = (L + a.chunk - 1) / a.chunk;
-  for (int e = threadIdx.x; e < G * D; e += blockDim.x) {
-    const int h = e / D, dim = e - h * D;
+  for (int e = threadIdx.x; e < G * (D / 4); e += blockDim.x) {
+    const int h = e / (D / 4), dim = 4 * (e - h * (D / 4));
     float M = -INFINITY;
-    for (int w = 0; w < nwaves; ++w) M = fmaxf(M, sm_m[w][h]);
-    float num = 0.f, den = 0.f;
-    if (M != -INFINITY) {
-      for (int w = 0; w < nwaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sm_m[w][h] - M);
-        num += f * ((const float*)(dyn + (size_t)w * wbytes))[h * (D + 1) + dim];
+#pragma unroll
+    for (int w = 0; w < kMaxWaves; ++w) M = fmaxf(M, sm_m[min(w, nwaves - 1)][h]);
+    f32x4_t num = {0.f, 0.f, 0.f, 0.f};
+    float den = 0.f;
+    for (int w0 = 0; w0 < nwaves; w0 += 4)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int w = min(w0 + i, nwaves - 1);
+        const float f = w0 + i < nwaves && M != -INFINITY ? __builtin_amdgcn_exp2f(sm_m[w][h] - M) : 0.f;
+        num += f * *(const f32x4_t*)(dyn + (size_t)w * wbytes + (h * (D + 4) + dim) * 4);
         den += f * sm_l[w][h];
       }
-    }
     const size_t bh = (size_t)b * hq + g * G + h;
     if (nsp == 1) {
-      write_final(a, bh, D, dim, M, num, den);
+      const f32x4_t y = den > 0.f ? num / den : f32x4_t{0.f, 0.f, 0.f, 0.f};
+      *(f32x4_a4_t*)(a.out + bh * D + dim) = y;
+      if (a.lse && dim == 0) a.lse[bh] = den > 0.f ? (M + log2f(den)) * kLn2 : -INFINITY;
     } else {
       const size_t pidx = bh * a.nsplit + split;
-      a.part_o[pidx * D + dim] = num;
+      *(f32x4_a4_t*)(a.part_o + pidx * D + dim) = num;
       if (dim == 0) {
         a.part_ml[pidx * 2] = M;
         a.part_ml[pidx * 2 + 1] = den;
@@ -481,16 +487,18 @@ void split_geometry(long long units, int rows_cap, int* chunk, int* nsplit) {
 // Waves of a workgroup, one for each tile at most: eight where it has a CU to
 // itself (8 units of 256 rows 7.8, with four 8.4, 256 of 4800 62.3 and 64.7) and for
 // long streams (1024 units of 16384 rows at d 64 323 and 338), else four (512 of
-// 600 rows 22.1, with eight 25.5).
-int waves_for(long long groups, int chunk) {
+// 600 rows 22.1, with eight 25.5).  Short streams of many heads take waves for
+// joining the heads' rows too (64 units of 16 heads and 7 rows 7.3 with four waves,
+// 10.2 with one; 512 of 4 heads and 64 rows 7.4 with their two, 7.9 with four).
+int waves_for(long long groups, int chunk, int outputs) {
   const int most = groups <= kCus || chunk > 8192 ? kMaxWaves : 4;
-  return std::min(most, chunk / kTile);
+  return std::min(most, std::max(chunk / kTile, std::min(4, outputs / 512)));
 }
 
 template <int D, bool DENSE, bool PAGED, int QP, bool WIDE>
 hipError_t launch_typed(QuantArgs& a, hipStream_t stream) {
   const int units = a.kv.batch * a.kv.hkv, G = a.kv.hq / a.kv.hkv;
-  const int waves = waves_for((long long)units * a.nsplit, a.chunk);
+  const int waves = waves_for((long long)units * a.nsplit, a.chunk, G * D);
   // long whole streams on more units than CUs, which take another as they end
   // (64 ragged sequences of 8k to 16k, 8 kv heads: 259 us in index order, 246)
   a.by_length = DENSE && a.nsplit == 1 && units > kCus && a.chunk > 8192 && a.kv.batch > 1 && a.kv.batch <= 1024;
