@@ -555,19 +555,20 @@ __global__ __launch_bounds__(kThreads) void select_blocks(BlockArgs a) {
   pick_row(a, m, u, kb, keys, s_list, s);
 }
 
-// One launch (us, then in two): where a workgroup reads a row in about what the
-// second launch costs (8 rows of 128 KB 8.6 and 10.3, of 512 KB 16.3 and 11.1), in
-// half of the CUs for longer rows (128 of 256 KB 13.6 and 14.7, of 2 MB 65 and
-// 58.7), and where the rows fill the CUs (192 of 1 MB 44.6 and 49.3, 256 of 2 MB
-// 104.5 and 108, 512 of 512 KB 54.3 and 64.2; 256 of 8 MB 404 and 384), but for long
-// rows of a few more units than CUs, which wait for the CUs that take two (320 of
-// 2 MB 145 and 140, paged 169 and 151, of 512 KB 40.2 and 43.3).
+// One launch (us, then in two; d 128 in bf16): where a workgroup reads a row in
+// about what the second launch costs (8 rows of 192 KB 9.7 and 10.4, of 256 KB 11.5
+// and 10.5), up to as much longer rows as there are more of them (96 of 256 KB 13.0
+// and 13.8, of 512 KB 19.5 and 18.0; 160 of 512 KB 22.5 and 23.9, of 1 MB 39.5 and
+// 38.9), and where the rows fill the CUs (192 of 1 MB 42.6 and 43.1, 256 of 2 MB 101
+// and 107, 512 of 512 KB 52.8 and 59.1, ragged 42.1 and 48.1; 256 of 8 MB 404 and
+// 384), but for long rows of a few more units than CUs, which wait for the CUs that
+// take two (264 of 512 KB 37.5 and 35.1, 320 of 2 MB 143 and 125; 384 of 512 KB 43.2
+// and 46.1, of 2 MB 150 and 148).
 bool one_launch(long long units, long long row_bytes) {
   constexpr long long KB = 1024;
-  if (row_bytes <= 128 * KB) return true;
-  if (units < 96) return false;
-  if (units < 192) return row_bytes <= 512 * KB;
-  return row_bytes <= (units > 256 && units < 448 ? 768 * KB : 4096 * KB);
+  if (row_bytes <= 192 * KB) return true;
+  if (units < 192) return row_bytes < 4 * KB * units;
+  return row_bytes <= (units > 256 && units < 384 ? 384 * KB : 4096 * KB);
 }
 
 // Dynamic LDS beyond the default: always the same bound, so that calls of other

@@ -452,27 +452,25 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
 // Splits of a unit and rows of a split, a multiple of the tile.  Times in us, d 128
 // with 4 heads a kv head where nothing else is said.
 // Up to 256 units: one workgroup per CU, but no split of few rows, which saves
-// the merge launch (8 units of 600 rows 9.9 whole, 11.6 in six; of 1200 17.3 and
-// 11.6; 96 units of 1200 rows 15.5 whole, 16.6 in two; of 2400 23.4 and 22.3), no
-// split below kMinSplit rows, and three of long rows where that leaves a third of
-// the CUs idle (160 units of 4096 rows 40.9 in three, 41.6 whole, at d 64 of 16384
-// 62.8 and 106; 200 units of 16384 rows 147.5 whole, 158 in six).
+// the merge launch (8 units of 600 rows 9.6 whole, 11.0 in four; of 1000 11.8 and
+// 11.1; 96 units of 1200 rows 15.3 whole, 15.8 in two; of 2400 23.2 and 20.9), no
+// split below kMinSplit rows, and of the units that leave CUs idle only long ones
+// that fill two workgroups a CU in three (136 units of 12000 rows 79.0 whole, 73.5
+// in three, of ragged 16384 92.8 and 78.9; 160 of 4096 31.4 and 34.3; 176 of 8192
+// 58.0 and 76.5).
 // More units than CUs: whole, as the workgroups of a CU share it (512 of 16384 rows
-// 330, in two 338), but long rows of a few more units than CUs, which wait for the
-// CUs that take two (288 of 16384 rows 251 whole, 216 in four; 384 291 and 281).
+// 326, in two 334), but long rows of a few more units than CUs, which wait for the
+// CUs that take two (264 of 4096 rows 61.4 whole, 54.7 in four; 320 of 16384 244
+// and 215; 384 of 16384 262 and 255).
 constexpr long long kCus = 256;
-constexpr int kWholeFew = 768, kWholeMany = 1536, kFewUnits = 64;
+constexpr int kWholeFew = 850, kWholeMany = 1536, kFewUnits = 64;
 constexpr int kMinSplit = 128;
-constexpr long long kThirdIdle = 176;
 constexpr int kLongRows = 4000;
 
 long long splits_of(long long units, long long rows) {
-  if (units > kCus) {
-    if (units <= 320 && rows >= kLongRows) return 4;
-    return units < 448 && rows >= 2 * kLongRows ? 2 : 1;
-  }
+  if (units > kCus) return units <= 320 && rows >= kLongRows ? 4 : 1;
   if (rows <= (units > kFewUnits ? kWholeMany : kWholeFew)) return 1;
-  const long long k = units > kCus / 2 && units <= kThirdIdle && rows >= kLongRows ? 3 : kCus / units;
+  const long long k = units > kCus / 2 && 3 * units <= 2 * kCus && rows >= 2 * kLongRows ? 3 : kCus / units;
   return std::max(1LL, std::min(k, rows / kMinSplit));
 }
 
@@ -485,11 +483,12 @@ void split_geometry(long long units, int rows_cap, int* chunk, int* nsplit) {
 }
 
 // Waves of a workgroup, one for each tile at most: eight where it has a CU to
-// itself (8 units of 256 rows 7.8, with four 8.4, 256 of 4800 62.3 and 64.7) and for
-// long streams (1024 units of 16384 rows at d 64 323 and 338), else four (512 of
-// 600 rows 22.1, with eight 25.5).  Short streams of many heads take waves for
-// joining the heads' rows too (64 units of 16 heads and 7 rows 7.3 with four waves,
-// 10.2 with one; 512 of 4 heads and 64 rows 7.4 with their two, 7.9 with four).
+// itself (256 units of 600 rows 13.1, with four 13.3, with two 16.5) and for long
+// streams (64 ragged sequences of up to 16384 rows, 8 kv heads, in length order 248
+// us, with four 264, of equal lengths 331 and 330), else four (512 of 600 rows 20.0,
+// with eight 22.6).  Short streams of many heads take waves for joining the heads'
+// rows too (64 units of 16 heads and 7 rows 7.3 with four waves, 10.2 with one; 512
+// of 4 heads and 64 rows 7.4 with their two, 7.9 with four).
 int waves_for(long long groups, int chunk, int outputs) {
   const int most = groups <= kCus || chunk > 8192 ? kMaxWaves : 4;
   return std::min(most, std::max(chunk / kTile, std::min(4, outputs / 512)));
@@ -500,7 +499,8 @@ hipError_t launch_typed(QuantArgs& a, hipStream_t stream) {
   const int units = a.kv.batch * a.kv.hkv, G = a.kv.hq / a.kv.hkv;
   const int waves = waves_for((long long)units * a.nsplit, a.chunk, G * D);
   // long whole streams on more units than CUs, which take another as they end
-  // (64 ragged sequences of 8k to 16k, 8 kv heads: 259 us in index order, 246)
+  // (64 ragged sequences of 8k to 16k, 8 kv heads: 260 us in index order, 248; of
+  // equal lengths 326 and 331)
   a.by_length = DENSE && a.nsplit == 1 && units > kCus && a.chunk > 8192 && a.kv.batch > 1 && a.kv.batch <= 1024;
   const size_t dyn = (size_t)waves * wave_bytes(D, G) + query_bytes(D, QP);
   if (dyn > 49152) {
@@ -547,12 +547,12 @@ size_t quant_attn_call_bytes(int batch, int hq, int hkv, int d, int rows_cap) {
 }
 
 // A call of fewer sequences may split its units more: up to 256 units have at
-// most 3 x 176 splits in all, up to 320 four each and up to 447 two, all others
-// one, so that many partials of hq / hkv heads hold every smaller call.
+// most 512 splits in all, up to 320 four each, all others one, so that many
+// partials of hq / hkv heads hold every smaller call.
 size_t quant_attn_workspace_bytes(int batch, int hq, int hkv, int d, int rows_cap) {
   const long long units = (long long)batch * hkv;
   const long long groups = std::max(units, units > kCus ? 4 * std::min(units, 320LL)
-                                                        : std::max(kCus, 3 * std::min(units, kThirdIdle)));
+                                                        : std::max(kCus, std::min(3 * units, 2 * kCus)));
   const long long per = units > 0 ? (groups + units - 1) / units : 0;
   return std::max(attn_layout(batch, hq, d, (int)per).total,
                   quant_attn_call_bytes(batch, hq, hkv, d, rows_cap));
