@@ -169,11 +169,64 @@ __device__ __forceinline__ f16x8_t f16_of_e4m3(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(f16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
+// The query operands, of product kk dims grp D/4 + 8 kk .. +7 of a lane's head.
+// bf16: in registers.
+template <int D, int QP>
+struct Query {
+  bf16x8_t f[D / 32];
+
+  __device__ __forceinline__ void load(const void* q, size_t at, int, bool on) {
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) {
+      const u32x4_t v = *(const u32x4_a2_t*)((const __bf16*)q + at + 8 * kk);
+      f[kk] = __builtin_bit_cast(bf16x8_t, on ? v : u32x4_t{0u, 0u, 0u, 0u});
+    }
+  }
+  __device__ __forceinline__ void stage(const void*, size_t, int, int, int, bool, u32x4_t*) {}
+  __device__ __forceinline__ bf16x8_t part(int, int kk, const u32x4_t*, int) const { return f[kk]; }
+};
+
+// fp32: in three bf16 parts (24 bits) in LDS, product kk by wave kk; a barrier
+// follows (all products by every wave, without one: 7 units of 16 heads and 11312
+// rows 16.0 us, 15.2 so).
+template <int D>
+struct Query<D, 3> {
+  float4 x, y;   // of product wave mod D / 32
+
+  __device__ __forceinline__ void load(const void* q, size_t at, int wave, bool) {
+    x = load_f32x4((const float*)q + at + 8 * (wave % (D / 32)));
+    y = load_f32x4((const float*)q + at + 8 * (wave % (D / 32)) + 4);
+  }
+  __device__ __forceinline__ void stage(const void* q, size_t at, int wave, int nwaves, int lane, bool on,
+                                        u32x4_t* s_q) {
+    for (int kk = wave % (D / 32);;) {
+      float r[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+        bf16x8_t h;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h[i] = (__bf16)(on ? r[i] : 0.f);
+          r[i] -= (float)h[i];
+        }
+        s_q[(part * (D / 32) + kk) * 64 + lane] = __builtin_bit_cast(u32x4_t, h);
+      }
+      kk += nwaves;
+      if (kk >= D / 32) break;
+      x = load_f32x4((const float*)q + at + 8 * kk);
+      y = load_f32x4((const float*)q + at + 8 * kk + 4);
+    }
+  }
+  __device__ __forceinline__ bf16x8_t part(int p, int kk, const u32x4_t* s_q, int lane) const {
+    return __builtin_bit_cast(bf16x8_t, s_q[(p * (D / 32) + kk) * 64 + lane]);
+  }
+};
+
 // Lane (col, grp) owns query head col (with !WIDE col mod 8) and in the V product
 // the rows 16 s + 4 grp + e of the tile, in the order 4 s + e.
 template <int D, int QP, bool WIDE>
 __device__ __forceinline__ void consume_tile(uint32_t ok, WaveState<D>& st,
-                                             const bf16x8_t (&qf)[D / 32], const u32x4_t* s_q,
+                                             const Query<D, QP>& q, const u32x4_t* s_q,
                                              const u32x4_t* s_k, const u32x4_t* s_v, const float* s_sc,
                                              int lane) {
   constexpr int CH = D / 16;
@@ -191,14 +244,9 @@ __device__ __forceinline__ void consume_tile(uint32_t ok, WaveState<D>& st,
       for (int h = 0; h < 2; ++h) {
         const int kk = 2 * i + h;
         const bf16x8_t kf = bf16_of_e4m3(c[2 * h], c[2 * h + 1]);
-        if constexpr (QP == 1) {
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[kk], acc, 0, 0, 0);
-        } else {
 #pragma unroll
-          for (int part = QP - 1; part >= 0; --part)   // small parts first
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                kf, __builtin_bit_cast(bf16x8_t, s_q[(part * (D / 32) + kk) * 64 + lane]), acc, 0, 0, 0);
-        }
+        for (int part = QP - 1; part >= 0; --part)   // small parts first
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q.part(part, kk, s_q, lane), acc, 0, 0, 0);
       }
     }
     const float4 ks = *(const float4*)(s_sc + 16 * s + 4 * grp);
@@ -259,35 +307,6 @@ __device__ __forceinline__ void consume_tile(uint32_t ok, WaveState<D>& st,
   }
 }
 
-// The query operand of product kk: dims grp D/4 + 8 kk .. +7 of its head; fp32 in
-// three bf16 parts (24 bits), to LDS.
-template <int D, int QP>
-__device__ __forceinline__ void load_query(const void* q, size_t bh, bool on, int grp, int lane,
-                                           bf16x8_t (&qf)[D / 32], u32x4_t* s_q) {
-#pragma unroll
-  for (int kk = 0; kk < D / 32; ++kk) {
-    const size_t at = bh * D + grp * (D / 4) + 8 * kk;
-    if constexpr (QP == 1) {
-      const u32x4_t v = *(const u32x4_a2_t*)((const __bf16*)q + at);
-      qf[kk] = __builtin_bit_cast(bf16x8_t, on ? v : u32x4_t{0u, 0u, 0u, 0u});
-    } else {
-      const float4 x = load_f32x4((const float*)q + at), y = load_f32x4((const float*)q + at + 4);
-      float r[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int part = 0; part < QP; ++part) {
-        bf16x8_t h;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          h[i] = (__bf16)(on ? r[i] : 0.f);
-          r[i] -= (float)h[i];
-        }
-        // every wave writes the same values
-        s_q[(part * (D / 32) + kk) * 64 + lane] = __builtin_bit_cast(u32x4_t, h);
-      }
-    }
-  }
-}
-
 template <int D, bool DENSE, bool PAGED, int QP, bool WIDE>
 __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) {
   // dynamic LDS: per-wave regions, then the query operands of fp32 queries
@@ -335,14 +354,16 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
   rows.base = (b * hkv + g) * a.kv.capacity;
   rows.table = PAGED ? a.kv.table + (int64_t)b * a.kv.max_pages : nullptr;
   rows.last_page = a.kv.max_pages - 1;
+  Query<D, QP> query;
+  const int head = WIDE ? col : col & 7;
+  const size_t q_at = ((size_t)b * hq + g * G + (head < G ? head : 0)) * D + grp * (D / 4);
+  query.load(a.q, q_at, wave, head < G);
   Tile<D> T;
   if (DENSE && a.kv.max_seq_len > 0) {
     const int p = min(t, a.kv.max_seq_len - 1);
     load_tile<D>(T, a, rows.row(rows.page(p), p), lane);
   }
-  bf16x8_t qf[D / 32];
-  const int head = WIDE ? col : col & 7;
-  load_query<D, QP>(a.q, (size_t)b * hq + g * G + (head < G ? head : 0), head < G, grp, lane, qf, s_q);
+  query.stage(a.q, q_at, wave, nwaves, lane, head < G, s_q);
   const int nb = kv_seq_len(a.kv, b);
   if (!DENSE && unit_excluded(a, u)) return;
   rows.sp = unit_span<DENSE>(a, u, b, nb);
@@ -363,6 +384,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
   st.r = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (QP > 1) lds_barrier();   // the query is in LDS
   const int ntiles = (end - start + kTile - 1) / kTile;
   // (no page of an empty sequence is looked up: its table may be empty too)
   const int iters = nb > 0 && wave < ntiles ? (ntiles - wave + nwaves - 1) / nwaves : 0;
@@ -395,7 +417,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
 #pragma unroll
         for (int blk = 0; blk < D / 16; ++blk) st.o[blk] *= f;
       }
-      consume_tile<D, QP, WIDE>(ok, st, qf, s_q, s_k, s_v, s_sc, lane);
+      consume_tile<D, QP, WIDE>(ok, st, query, s_q, s_k, s_v, s_sc, lane);
     }
   }
 
