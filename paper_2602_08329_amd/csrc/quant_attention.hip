@@ -169,20 +169,21 @@ __device__ __forceinline__ f16x8_t f16_of_e4m3(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(f16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
-// The query operands, of product kk dims grp D/4 + 8 kk .. +7 of a lane's head.
-// bf16: in registers.
+// The query operands, of product kk dims grp D/4 + 8 kk .. +7 of a lane's head
+// (lanes without one take the first head's, to no effect).  bf16: in registers, not
+// touched before the first product, as a use waits for all earlier loads.
 template <int D, int QP>
 struct Query {
   bf16x8_t f[D / 32];
 
-  __device__ __forceinline__ void load(const void* q, size_t at, int, bool on) {
+  __device__ __forceinline__ void load(const void* q, size_t at, int) {
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) {
       const u32x4_t v = *(const u32x4_a2_t*)((const __bf16*)q + at + 8 * kk);
-      f[kk] = __builtin_bit_cast(bf16x8_t, on ? v : u32x4_t{0u, 0u, 0u, 0u});
+      f[kk] = __builtin_bit_cast(bf16x8_t, v);
     }
   }
-  __device__ __forceinline__ void stage(const void*, size_t, int, int, int, bool, u32x4_t*) {}
+  __device__ __forceinline__ void stage(const void*, size_t, int, int, int, u32x4_t*) {}
   __device__ __forceinline__ bf16x8_t part(int, int kk, const u32x4_t*, int) const { return f[kk]; }
 };
 
@@ -193,11 +194,11 @@ template <int D>
 struct Query<D, 3> {
   float4 x, y;   // of product wave mod D / 32
 
-  __device__ __forceinline__ void load(const void* q, size_t at, int wave, bool) {
+  __device__ __forceinline__ void load(const void* q, size_t at, int wave) {
     x = load_f32x4((const float*)q + at + 8 * (wave % (D / 32)));
     y = load_f32x4((const float*)q + at + 8 * (wave % (D / 32)) + 4);
   }
-  __device__ __forceinline__ void stage(const void* q, size_t at, int wave, int nwaves, int lane, bool on,
+  __device__ __forceinline__ void stage(const void* q, size_t at, int wave, int nwaves, int lane,
                                         u32x4_t* s_q) {
     for (int kk = wave % (D / 32);;) {
       float r[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
@@ -206,7 +207,7 @@ struct Query<D, 3> {
         bf16x8_t h;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          h[i] = (__bf16)(on ? r[i] : 0.f);
+          h[i] = (__bf16)r[i];
           r[i] -= (float)h[i];
         }
         s_q[(part * (D / 32) + kk) * 64 + lane] = __builtin_bit_cast(u32x4_t, h);
@@ -352,19 +353,22 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
   rows.num_pages = a.kv.num_pages;
   rows.shift = a.sc.block_shift;
   rows.base = (b * hkv + g) * a.kv.capacity;
-  rows.table = PAGED ? a.kv.table + (int64_t)b * a.kv.max_pages : nullptr;
-  rows.last_page = a.kv.max_pages - 1;
+  // (a table without entries is not read)
+  rows.table = PAGED && a.kv.max_pages > 0 ? a.kv.table + (int64_t)b * a.kv.max_pages : a.kv.seq_lens;
+  rows.last_page = max(a.kv.max_pages, 1) - 1;
   Query<D, QP> query;
   const int head = WIDE ? col : col & 7;
   const size_t q_at = ((size_t)b * hq + g * G + (head < G ? head : 0)) * D + grp * (D / 4);
-  query.load(a.q, q_at, wave, head < G);
+  query.load(a.q, q_at, wave);
   Tile<D> T;
   if (DENSE && a.kv.max_seq_len > 0) {
     const int p = min(t, a.kv.max_seq_len - 1);
     load_tile<D>(T, a, rows.row(rows.page(p), p), lane);
   }
-  query.stage(a.q, q_at, wave, nwaves, lane, head < G, s_q);
   const int nb = kv_seq_len(a.kv, b);
+  // the pages of a set's first entries before the lengths are known, as positions
+  // of the tail come last
+  int g0 = DENSE ? 0 : rows.page(raw0);
   if (!DENSE && unit_excluded(a, u)) return;
   rows.sp = unit_span<DENSE>(a, u, b, nb);
   const int L = rows.sp.L;
@@ -384,7 +388,10 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
   st.r = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  if (QP > 1) lds_barrier();   // the query is in LDS
+  if (QP > 1) {
+    query.stage(a.q, q_at, wave, nwaves, lane, s_q);
+    lds_barrier();
+  }
   const int ntiles = (end - start + kTile - 1) / kTile;
   // (no page of an empty sequence is looked up: its table may be empty too)
   const int iters = nb > 0 && wave < ntiles ? (ntiles - wave + nwaves - 1) / nwaves : 0;
@@ -394,7 +401,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
       T.ok &= (uint32_t)__builtin_amdgcn_ballot_w64(t < end);
     } else {
       const int p0 = rows.pos(raw0, t, end);
-      load_tile<D>(T, a, rows.row(rows.page(p0), p0), lane);
+      if (PAGED && __builtin_amdgcn_ballot_w64(p0 >= 0 && p0 != raw0)) g0 = rows.page(p0);
+      load_tile<D>(T, a, rows.row(g0, p0), lane);
     }
     int g1 = rows.page(p1);
     for (int i = 0; i < iters; ++i) {
