@@ -26,7 +26,7 @@
 // heads of d 128 (1.59 GB) 243 us, 6.5 TB/s, 8 of 4k with 32 kv heads (269 MB) 42
 // us, 6.4 TB/s, where a plain read reaches 7.1.  Few units are bound by the chain of
 // loads (list, page, row), the joining of the waves and the second launch: the
-// selected set of one 128k sequence (8 units of 2300 rows, 4.8 MB) 7.2 us and 3.5 in
+// selected set of one 128k sequence (8 units of 2300 rows, 4.8 MB) 7.1 us and 3.5 in
 // attn_merge.
 #include <algorithm>
 
