@@ -559,6 +559,7 @@ def test_block_select(hq, hkv, d, bs, paged, n, k, sink, window, dtype):
     (1, 2, 8750, 900, True, "bf16"),       # more keys than the picking workgroup's registers hold
     (2, 1, 9000, 80000, False, "f32"),     # more chosen blocks than its LDS holds
     (24, 8, 4300, 3000, False, "bf16"),    # one launch of long rows
+    (1, 2, 1500, 640, False, "bf16"), (1, 2, 3000, 900, True, "bf16"), (24, 8, 1500, 640, True, "bf16"),
     (96, 1, 300, 640, True, "bf16"), (96, 1, 600, 640, False, "f32"), (10, 32, 200, 640, False, "bf16"),
 ])
 def test_block_select_long_and_many_rows(batch, hkv, nb, k, paged, dtype):
