@@ -29,6 +29,7 @@
 // selected set of one 128k sequence (8 units of 2300 rows, 4.8 MB) 7.1 us and 3.5 in
 // attn_merge.
 #include <algorithm>
+#include <cmath>
 
 #include "attention_common.h"
 #include "prhs_internal.h"
@@ -481,13 +482,17 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
 
 // Splits of a unit and rows of a split, a multiple of the tile.  Times in us, d 128
 // with 4 heads a kv head where nothing else is said.
-// Up to 256 units: one workgroup per CU, but no split of few rows, which saves
-// the merge launch (8 units of 600 rows 9.6 whole, 11.0 in four; of 1000 11.8 and
-// 11.1; 96 units of 1200 rows 15.3 whole, 15.8 in two; of 2400 23.2 and 20.9), no
-// split below kMinSplit rows, and of the units that leave CUs idle only long ones
-// that fill two workgroups a CU in three (136 units of 12000 rows 79.0 whole, 73.5
-// in three, of ragged 16384 92.8 and 78.9; 160 of 4096 31.4 and 34.3; 176 of 8192
-// 58.0 and 76.5).
+// Up to 256 units: one workgroup of eight waves a CU (64 units of ragged 16384 rows
+// 38.9, two of four waves 43.9), two where that fills the CUs better (96 units of
+// ragged 16384 rows in two 60.8, in five 56.0; 72 of 1600 in three 14.2, in seven
+// 13.8), but no more splits than is worth their joining, each 0.05 (one unit of
+// 32768 rows in 256 22.3, in 64 14.4, of 131072 26.1, in 128 21.3), so that their
+// number grows with the root of the rows.  No split of few rows, which saves the
+// merge launch (8 units of 600 rows 9.6 whole, 11.0 in four; of 1000 11.8 and 11.1;
+// 96 units of 1600 rows 16.2 whole, 15.4 in five, as sets 17.0 and 17.1; 120 16.3
+// and 16.9), no split below kMinSplit rows, and of more than 128 units only long
+// ones (136 of 12000 rows 79.0 whole, 73.5 in three, of ragged 16384 92.8 and 78.9;
+// 160 of 4096 31.4 and 34.3).
 // More units than CUs: whole, as the workgroups of a CU share it (512 of 16384 rows
 // 326, in two 334), but long rows of a few more units than CUs, which wait for the
 // CUs that take two (264 of 4096 rows 61.4 whole, 54.7 in four; 320 of 16384 244
@@ -500,8 +505,11 @@ constexpr int kLongRows = 4000;
 long long splits_of(long long units, long long rows) {
   if (units > kCus) return units <= 320 && rows >= kLongRows ? 4 : 1;
   if (rows <= (units > kFewUnits ? kWholeMany : kWholeFew)) return 1;
-  const long long k = units > kCus / 2 && 3 * units <= 2 * kCus && rows >= 2 * kLongRows ? 3 : kCus / units;
-  return std::max(1LL, std::min(k, rows / kMinSplit));
+  if (units > kCus / 2 && rows < 2 * kLongRows) return 1;
+  long long k = kCus / units;
+  if (units > kFewUnits && 2 * kCus / units > 2 * k) k = 2 * kCus / units;
+  const long long join = std::max(32LL, (long long)std::sqrt(rows / 16.0));
+  return std::max(1LL, std::min({k, join, rows / kMinSplit}));
 }
 
 void split_geometry(long long units, int rows_cap, int* chunk, int* nsplit) {
@@ -576,13 +584,13 @@ size_t quant_attn_call_bytes(int batch, int hq, int hkv, int d, int rows_cap) {
   return attn_layout(batch, hq, d, nsplit).total;
 }
 
-// A call of fewer sequences may split its units more: up to 256 units have at
-// most 512 splits in all, up to 320 four each, all others one, so that many
-// partials of hq / hkv heads hold every smaller call.
+// A call of fewer sequences may split its units more: up to 64 units have at most
+// 256 splits in all, up to 256 units 512, up to 320 four each, all others one, so
+// that many partials of hq / hkv heads hold every smaller call.
 size_t quant_attn_workspace_bytes(int batch, int hq, int hkv, int d, int rows_cap) {
   const long long units = (long long)batch * hkv;
-  const long long groups = std::max(units, units > kCus ? 4 * std::min(units, 320LL)
-                                                        : std::max(kCus, std::min(3 * units, 2 * kCus)));
+  const long long most = units <= kFewUnits ? kCus : units <= kCus ? 2 * kCus : 4 * std::min(units, 320LL);
+  const long long groups = std::max(units, most);
   const long long per = units > 0 ? (groups + units - 1) / units : 0;
   return std::max(attn_layout(batch, hq, d, (int)per).total,
                   quant_attn_call_bytes(batch, hq, hkv, d, rows_cap));

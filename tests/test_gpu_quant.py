@@ -150,6 +150,11 @@ def test_dense_head_groups(hq, hkv):
     ((5000, 4999, 33, 2500), 8, 2, 64, False, "bf16"),
     ((2048, 2049), 16, 1, 128, False, "f32"),
     (tuple(700 - 3 * i for i in range(40)), 8, 8, 64, True, "bf16"),    # 320 units
+    ((70001,), 2, 1, 64, True, "bf16"),            # as many splits as the rows' root allows
+    (tuple(2000 - 7 * i for i in range(96)), 2, 1, 128, False, "bf16"),   # two workgroups a CU
+    (tuple(8001 - 50 * i for i in range(140)), 1, 1, 64, False, "f32"),   # three splits
+    (tuple(4001 - 9 * i for i in range(270)), 1, 1, 64, True, "bf16"),    # four
+    ((7, 0, 3), 32, 2, 128, True, "bf16"),         # more waves than tiles
 ])
 def test_dense_splits(lens, hq, hkv, d, paged, dtype):
     c = Cache(lens, hq, hkv, d, 16, paged, dtype, seed=lens[0])
