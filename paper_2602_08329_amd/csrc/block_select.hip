@@ -10,8 +10,8 @@
 //
 // Scores become order-preserving keys (0, below every number's key, for NaN and
 // for blocks whose page lies outside the pool).  The key of the last chosen block
-// comes from a radix search, then one pass in block order writes the chosen
-// blocks (which settles ties) and the set.  Two forms:
+// comes from histograms of narrowing intervals, then one pass in block order
+// writes the chosen blocks (which settles ties) and the set.  Two forms:
 //   select_blocks   one workgroup per (batch, kv head) scores its blocks into LDS
 //                   and picks: one launch;
 //   score_blocks    spreads the rows' scores over the chip, keys in the
