@@ -510,7 +510,10 @@ prhs_status prhs_quant_store(const prhs_quant_kv* kv, const void* k_new, const v
 /* prhs_sparse_decode_attn, prhs_reuse_decode_attn, prhs_dense_decode_attn and
  * prhs_pool_decode_attn over an 8-bit cache: same arguments, semantics and
  * outputs, with k_i = k_scale * k8_i and v_i = v_scale * v8_i of the block of
- * token i.  Products are accumulated in fp32; a weight times its v_scale keeps
+ * token i.  A NaN logit (a NaN element of an attended key, as the store keeps
+ * what is not finite, or of the query) makes out and lse of its head NaN, a NaN
+ * value its dim of out; neither reaches a head that does not attend it.
+ * Products are accumulated in fp32; a weight times its v_scale keeps
  * 22 bits, or 2^-32 of the largest weight times the largest v_scale met.
  * ws: >= prhs_workspace_size(PRHS_OP_QUANT_SPARSE_ATTN, set_cap) bytes, for
  * the dense form PRHS_OP_QUANT_DENSE_ATTN; no initialisation needed. */

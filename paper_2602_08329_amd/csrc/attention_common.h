@@ -214,11 +214,12 @@ __device__ __forceinline__ float sum_over_groups(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Writes out/lse of query head bh from (M, sum, unnormalised numerator).
+// Writes out/lse of query head bh from (M, sum, unnormalised numerator).  The
+// sum is 0 where no row was attended, and NaN where a logit was.
 __device__ __forceinline__ void write_final(const AttnArgs& a, size_t bh, int D, int dim, float M,
                                             float num, float den) {
-  a.out[bh * D + dim] = den > 0.f ? num / den : 0.f;
-  if (a.lse && dim == 0) a.lse[bh] = den > 0.f ? (M + log2f(den)) * kLn2 : -INFINITY;
+  a.out[bh * D + dim] = den == 0.f ? 0.f : num / den;
+  if (a.lse && dim == 0) a.lse[bh] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
 }
 
 // Combines the split partials of one query head (grid: batch * num_q_heads,
@@ -277,22 +278,23 @@ __global__ __launch_bounds__(256) void attn_merge(AttnArgs a) {
         o[k] = ok ? po[(size_t)s * D + dim] : 0.f;
       }
     }
-    // rescale the running sums to the new maximum of this thread
+    // rescale the running sums to the new maximum of this thread; a split whose
+    // logits are all NaN has the maximum -inf and the weight 0, which leaves its
+    // sums NaN
     float bm = mx;
 #pragma unroll
     for (int k = 0; k < kMergePerThread; ++k) bm = fmaxf(bm, m[k]);
-    if (bm != -INFINITY) {
-      const float r = __builtin_amdgcn_exp2f(mx - bm);
-      num *= r;
-      den *= r;
+    const float ref = bm == -INFINITY ? 0.f : bm;
+    const float r = __builtin_amdgcn_exp2f(mx - ref);
+    num *= r;
+    den *= r;
 #pragma unroll
-      for (int k = 0; k < kMergePerThread; ++k) {
-        const float f = __builtin_amdgcn_exp2f(m[k] - bm);
-        num += f * o[k];
-        den += f * l[k];
-      }
-      mx = bm;
+    for (int k = 0; k < kMergePerThread; ++k) {
+      const float f = __builtin_amdgcn_exp2f(m[k] - ref);
+      num += f * o[k];
+      den += f * l[k];
     }
+    mx = bm;
   }
   // block-wide maximum
   const float wm = wave_max(mx);

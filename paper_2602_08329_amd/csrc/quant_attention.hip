@@ -466,9 +466,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
       }
     const size_t bh = (size_t)b * hq + g * G + h;
     if (nsp == 1) {
-      const f32x4_t y = den > 0.f ? num / den : f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const f32x4_t y = den == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : num / den;
       *(f32x4_a4_t*)(a.out + bh * D + dim) = y;
-      if (a.lse && dim == 0) a.lse[bh] = den > 0.f ? (M + log2f(den)) * kLn2 : -INFINITY;
+      if (a.lse && dim == 0) a.lse[bh] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
     } else {
       const size_t pidx = bh * a.nsplit + split;
       *(f32x4_a4_t*)(a.part_o + pidx * D + dim) = num;
