@@ -514,7 +514,7 @@ prhs_status prhs_quant_store(const prhs_quant_kv* kv, const void* k_new, const v
  * what is not finite, or of the query) makes out and lse of its head NaN, a NaN
  * value its dim of out; neither reaches a head that does not attend it.
  * Products are accumulated in fp32; a weight times its v_scale keeps
- * 22 bits, or 2^-32 of the largest weight times the largest v_scale met.
+ * 24 bits, down to 2^-110 of the largest weight times the largest v_scale met.
  * ws: >= prhs_workspace_size(PRHS_OP_QUANT_SPARSE_ATTN, set_cap) bytes, for
  * the dense form PRHS_OP_QUANT_DENSE_ATTN; no initialisation needed. */
 prhs_status prhs_quant_sparse_decode_attn(const prhs_quant_kv* kv, const void* q,

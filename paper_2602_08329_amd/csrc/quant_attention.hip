@@ -4,14 +4,17 @@
 // One workgroup per (unit, split) walks a contiguous chunk of the list with an
 // online softmax; a unit of several splits is joined by attn_merge.
 //
-// e4m3 values are exact in bf16 and fp16, so both products run on MFMA without
-// rounding an operand: K as bf16 with q (fp32 queries as three bf16 parts), V as
-// fp16 with the weights w_i = p_i vs_i r, r a power of two that brings the
-// largest vs the wave has met to at most 2^7.  p stays below 2^8 (lazy
-// rescaling), so w is below 2^15, and as an fp16 pair hi + lo it keeps 22 bits,
-// or an absolute 2^-25: 2^-32 of the largest weight.  With at most 8 heads a kv
-// head, hi and lo are two columns of one product (the queries stand in the
-// columns twice), else two products.
+// e4m3 values are exact in bf16, so both products run on MFMA without rounding
+// an operand to less than fp32 holds: K with q (fp32 queries as three bf16 parts,
+// 24 bits), V with the weights w_i = p_i vs_i r, three bf16 parts as well, r a
+// power of two, at most 2^126, that brings the largest vs the wave has met to
+// [2^80, 2^81) (a normal one to 1 or more).  p stays below 2^8 (lazy rescaling), so
+// sums over 2^22 rows stay below 2^120, and the parts are normal numbers for w down
+// to 2^-110, which the largest weight exceeds 2^110 times at least.  (Two fp16 parts have too little range: beside a block whose
+// values are 2^20 times the others' they left about ten bits of the others' weights.
+// They cost a product less: one sequence of 617 tokens 8.8 us, 9.3 so.)
+// With at most 8 heads a kv head, two of the parts are two columns of one product
+// (the queries stand in the columns twice), else each part is a product.
 //
 // A wave walks tiles of 32 rows: lane l knows row l of its tile.  List entries
 // are read three tiles ahead, their pages two, K, V and scales one, into
@@ -38,9 +41,6 @@ namespace prhs {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_a2_t __attribute__((ext_vector_type(4), aligned(2)));
@@ -125,22 +125,22 @@ __device__ __forceinline__ void load_tile(Tile<D>& T, const QuantArgs& a, int ro
   }
 }
 
-// A loaded tile to the wave's LDS; rows that are not there get V = 0 and scales
-// of 0 (their K only reaches logits that are masked).
+// A loaded tile to the wave's LDS, its V scales times r; rows that are not there
+// get V = 0 and scales of 0 (their K only reaches logits that are masked).
 template <int D>
-__device__ __forceinline__ void stage_tile(const Tile<D>& T, float scale_log2, u32x4_t* s_k, u32x4_t* s_v,
-                                           float* s_sc, int lane) {
+__device__ __forceinline__ void stage_tile(const Tile<D>& T, float scale_log2, float r, u32x4_t* s_k,
+                                           u32x4_t* s_v, float* s_sc, int lane) {
   constexpr int CH = D / 16, RPI = 64 / CH;
 #pragma unroll
   for (int j = 0; j < Tile<D>::KL; ++j) {
-    const int r = j * RPI + lane / CH, slot = tile_slot<D>(r, lane % CH);
+    const int row = j * RPI + lane / CH, slot = tile_slot<D>(row, lane % CH);
     s_k[slot] = T.k[j];
-    s_v[slot] = T.ok == 0xFFFFFFFFu || ((T.ok >> r) & 1u) ? T.v[j] : u32x4_t{0u, 0u, 0u, 0u};
+    s_v[slot] = T.ok == 0xFFFFFFFFu || ((T.ok >> row) & 1u) ? T.v[j] : u32x4_t{0u, 0u, 0u, 0u};
   }
   if (lane < kTile) {
     const bool in = (T.ok >> lane) & 1u;
     s_sc[lane] = in ? T.ks * scale_log2 : 0.f;
-    s_sc[kTile + lane] = in ? T.vs : 0.f;
+    s_sc[kTile + lane] = in ? T.vs * r : 0.f;
   }
 }
 
@@ -148,7 +148,7 @@ template <int D>
 struct WaveState {
   float m, l;
   int ve;       // exponent bits of the largest V scale met
-  float r;      // 2^(6 - that exponent)
+  float r;      // 2^(80 - that exponent), at most 2^126
   f32x4_t o[D / 16];
 };
 
@@ -159,15 +159,6 @@ __device__ __forceinline__ bf16x8_t bf16_of_e4m3(uint32_t a, uint32_t b) {
   w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false));
   w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true));
   return __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
-}
-
-__device__ __forceinline__ f16x8_t f16_of_e4m3(uint32_t a, uint32_t b) {
-  uint32_t w[4];
-  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false));
-  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true));
-  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false));
-  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true));
-  return __builtin_bit_cast(f16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
 // The query operands, of product kk dims grp D/4 + 8 kk .. +7 of a lane's head
@@ -262,11 +253,10 @@ __device__ __forceinline__ void consume_tile(uint32_t ok, WaveState<D>& st,
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) mt = fmaxf(mt, x[j]);
-  mt = max_over_groups(mt);
   // lazy rescaling: the reference st.m moves only when some head of the wave sees
   // its maximum rise by more than 2^8
-  const float m_new = fmaxf(st.m, mt);
-  if (__builtin_amdgcn_ballot_w64(m_new > st.m + 8.f)) {
+  if (__builtin_amdgcn_ballot_w64(mt > st.m + 8.f)) {
+    const float m_new = fmaxf(st.m, max_over_groups(mt));
     const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
     st.m = m_new;
     st.l *= alpha;
@@ -283,19 +273,31 @@ __device__ __forceinline__ void consume_tile(uint32_t ok, WaveState<D>& st,
   for (int j = 0; j < 8; ++j) {
     const float p = __builtin_amdgcn_exp2f(x[j] - mref);
     st.l += p;
-    w[j] = p * (vse[j] * st.r);
+    w[j] = p * vse[j];
   }
-  uint32_t hi[4], lo[4];
+  // The parts of w are its upper eight significant bits, the next eight and the
+  // rest, each the upper half of an fp32 word.  Not WIDE: one product with the first
+  // in columns 0 .. 7 and the second in 8 .. 15, where lanes take the first off
+  // beforehand, and another with the third in columns 8 .. 15.
+  constexpr uint32_t kUpper = 0xFFFF0000u;
+  constexpr int NP = WIDE ? 3 : 2;
+  const uint32_t off = !WIDE && col >= 8 ? kUpper : 0u;
+  const uint32_t last = WIDE || col >= 8 ? 0x07060302u : 0x0C0C0C0Cu;   // upper halves, zeros
+  bf16x8_t part[NP];
+  if (!WIDE)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const f16x2_t h = __builtin_convertvector(f32x2_t{w[2 * i], w[2 * i + 1]}, f16x2_t);
-    hi[i] = __builtin_bit_cast(uint32_t, h);
-    lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-        f32x2_t{w[2 * i] - (float)h[0], w[2 * i + 1] - (float)h[1]}, f16x2_t));
-    if (!WIDE) hi[i] = col < 8 ? hi[i] : lo[i];
+    for (int j = 0; j < 8; ++j) w[j] -= __uint_as_float(__float_as_uint(w[j]) & off);
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      u[i] = __builtin_amdgcn_perm(__float_as_uint(w[2 * i + 1]), __float_as_uint(w[2 * i]),
+                                   k == NP - 1 ? last : 0x07060302u);
+    part[k] = __builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3]));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] -= __uint_as_float(__float_as_uint(w[j]) & kUpper);
   }
-  const f16x8_t whi = __builtin_bit_cast(f16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-  const f16x8_t wlo = __builtin_bit_cast(f16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
   // lane `col` of a group addresses 8 dims of the group's row col / 2 (in the
   // order of w) and receives dim 16 blk + col of its 8 rows
   const int vr = 16 * (col >> 3) + 4 * grp + ((col >> 1) & 3);
@@ -303,9 +305,10 @@ __device__ __forceinline__ void consume_tile(uint32_t ok, WaveState<D>& st,
   for (int blk = 0; blk < D / 16; ++blk) {
     const uint8_t* at = (const uint8_t*)(s_v + tile_slot<D>(vr, blk)) + 8 * (col & 1);
     const i32x2_t t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t*)at);
-    const f16x8_t v = f16_of_e4m3((uint32_t)t[0], (uint32_t)t[1]);
-    st.o[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, whi, st.o[blk], 0, 0, 0);
-    if (WIDE) st.o[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, wlo, st.o[blk], 0, 0, 0);
+    const bf16x8_t v = bf16_of_e4m3((uint32_t)t[0], (uint32_t)t[1]);
+#pragma unroll
+    for (int k = NP - 1; k >= 0; --k)   // small parts first
+      st.o[blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, part[k], st.o[blk], 0, 0, 0);
   }
 }
 
@@ -409,23 +412,26 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
     for (int i = 0; i < iters; ++i) {
       const uint32_t ok = T.ok;
       const uint32_t vs = (ok >> (lane & (kTile - 1))) & 1u ? __float_as_uint(T.vs) & 0x7FFFFFFFu : 0u;
-      const int ve = max((int)(wave_umax(vs) >> 23), 1);
+      if (__builtin_amdgcn_ballot_w64(max((int)(vs >> 23), 1) > st.ve)) {   // a larger V scale than any before
+        const int ve = max((int)(wave_umax(vs) >> 23), 1);
+        const int re = min(334 - ve, 253);
+        // (the ratio of both r may be no fp32 number)
+        const int by = st.ve > 0 ? re - (int)(__float_as_uint(st.r) >> 23) : 0;
+        st.ve = ve;
+        st.r = __uint_as_float((uint32_t)re << 23);
+#pragma unroll
+        for (int blk = 0; blk < D / 16; ++blk)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st.o[blk][i] = __builtin_amdgcn_ldexpf(st.o[blk][i], by);
+      }
       __builtin_amdgcn_wave_barrier();
-      stage_tile<D>(T, a.scale_log2, s_k, s_v, s_sc, lane);
+      stage_tile<D>(T, a.scale_log2, st.r, s_k, s_v, s_sc, lane);
       __builtin_amdgcn_wave_barrier();
       load_tile<D>(T, a, rows.row(g1, p1), lane);
       p1 = rows.pos(raw2, t + 2 * step, end);
       g1 = rows.page(p1);
       raw2 = any ? rows.entry(t + 3 * step) : -1;
       t += step;
-      if (ve > st.ve) {   // a larger V scale than any before
-        const float r = __uint_as_float((uint32_t)min(max(260 - ve, 1), 253) << 23);
-        const float f = st.ve > 0 ? r / st.r : 1.f;
-        st.ve = ve;
-        st.r = r;
-#pragma unroll
-        for (int blk = 0; blk < D / 16; ++blk) st.o[blk] *= f;
-      }
       consume_tile<D, QP, WIDE>(ok, st, query, s_q, s_k, s_v, s_sc, lane);
     }
   }
@@ -441,7 +447,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
 #pragma unroll
   for (int blk = 0; blk < D / 16; ++blk) {
     f32x4_t v = st.o[blk] * unscale;
-    if (!WIDE)   // hi and lo: columns 8 apart
+    if (!WIDE)   // parts 8 columns apart
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = add_rotated<0x128>(v[i]);
     if (col < G) *(f32x4_t*)(wo + 16 * blk) = v;
