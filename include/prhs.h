@@ -569,7 +569,10 @@ prhs_status prhs_block_workspace_size(const prhs_kv* kv, const prhs_bounds* boun
  *   the candidates are the blocks that hold a position of the middle range;
  *   sigma_j = max over the group's query heads h of
  *     sum_d max(q[b][h][d] k_min[j][d], q[b][h][d] k_max[j][d])  (fp32),
- *     which no key of block j exceeds in q . k;
+ *     which no key that the bounds were made of exceeds in q . k (but for
+ *     fp32 rounding).  An 8-bit cache's bounds are of the keys as given: a
+ *     stored key of block j may exceed sigma_j by its rounding, at most
+ *     sum_d |q_d| (2^-4 max(|k_min|, |k_max|) + 2^-9 k_scale);
  *   the min(ceil(k_b / block_size), candidates) blocks of largest sigma are
  *   chosen, ties going to the lower block;
  *   blk_idx[b][g][0 .. blk_len) = the chosen blocks, ascending;

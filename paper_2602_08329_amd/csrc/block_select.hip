@@ -1,8 +1,9 @@
 // Selection of whole blocks by their key bounds.  With q+ = max(q, 0) and
 // q- = min(q, 0),
 //   sum_d max(q kmin, q kmax) = q+ . kmax + q- . kmin,
-// an upper bound of q . k over the block's keys: a product of length 2d, on MFMA
-// for bf16 and in vector fp32 for fp32 bounds.  What bounds it is reading the
+// an upper bound of q . k over the keys that the bounds were made of (for an 8-bit
+// cache those given to the store, which rounds them to 4 bits): a product of length
+// 2d, on MFMA for bf16 and in vector fp32 for fp32 bounds.  What bounds it is reading the
 // bounds (4d bytes a block in bf16) once: 512 rows of 4096 blocks at d 128 (1.07
 // GB) 181 us, 5.9 TB/s, where a kernel that only loads them in the same order
 // takes 150.  The scoring without its arithmetic takes the same time; the pick
