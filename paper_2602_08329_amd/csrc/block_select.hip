@@ -572,6 +572,21 @@ bool one_launch(long long units, long long row_bytes) {
   return row_bytes <= (units > 256 && units < 384 ? 384 * KB : 4096 * KB);
 }
 
+// The launches of `units` rows of nbmax keys and row_bytes of bounds: select_blocks,
+// or score_blocks in `chunks` workgroups a row, about four workgroups a CU, each of
+// whole rounds of its waves' tiles (`round` candidates).
+struct Shape {
+  bool one;
+  int chunk, chunks;
+};
+Shape launch_shape(long long units, int nbmax, long long row_bytes, int round) {
+  if (nbmax <= kLdsKeys && one_launch(units, row_bytes)) return {true, nbmax, 1};
+  const long long want = std::max(1LL, 1024 / std::max(1LL, units));
+  const long long rounds = ((nbmax + want - 1) / want + round - 1) / round;
+  const int chunk = (int)std::min((long long)(kLdsKeys / round), std::max(1LL, rounds)) * round;
+  return {false, chunk, (nbmax + chunk - 1) / chunk};
+}
+
 // Dynamic LDS beyond the default: always the same bound, so that calls of other
 // sizes on other threads do not lower it.
 constexpr int kMaxDynamicLds = 144 * 1024;
@@ -602,8 +617,8 @@ hipError_t launch_typed(BlockArgs& a, hipStream_t stream) {
   const int units = a.kv.batch * a.kv.hkv;
   constexpr size_t kScoreLds = S::kLdsQuery + (size_t)kWaves * S::kLdsWave;
   a.lds_list = (std::min(std::min(a.blk_cap, a.nbmax), kListMax) + 3) & ~3;
-  const long long row_bytes = (long long)a.nbmax * 2 * D * sizeof(T);
-  if (a.nbmax <= kLdsKeys && one_launch(units, row_bytes)) {
+  const Shape shape = launch_shape(units, a.nbmax, (long long)a.nbmax * 2 * D * sizeof(T), S::kRows * kWaves);
+  if (shape.one) {
     const size_t lds = ((size_t)a.nbmax + a.lds_list) * 4 + kScoreLds;
     auto launch = [&](auto r) {
       constexpr int R = decltype(r)::value;
@@ -614,18 +629,12 @@ hipError_t launch_typed(BlockArgs& a, hipStream_t stream) {
     };
     return with_keys(a.nbmax, kThreads, launch);
   }
-  // about four workgroups a CU, of whole rounds of their waves' tiles
-  constexpr int round = S::kRows * kWaves;
-  const int want = std::max(1, 1024 / std::max(1, units));
-  a.chunk = std::min(kLdsKeys / round, std::max(1, ((a.nbmax + want - 1) / want + round - 1) / round)) * round;
-  const int chunks = (a.nbmax + a.chunk - 1) / a.chunk;
-  if (chunks > 0) {
-    const size_t lds = kScoreLds + (size_t)a.chunk * 4;
-    const hipError_t e = allow_lds(score_blocks<T, D, PAGED>, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((score_blocks<T, D, PAGED>), dim3((unsigned)units * chunks), dim3(kThreads), lds,
-                       stream, a, chunks);
-  }
+  a.chunk = shape.chunk;
+  const size_t lds = kScoreLds + (size_t)a.chunk * 4;
+  const hipError_t e = allow_lds(score_blocks<T, D, PAGED>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((score_blocks<T, D, PAGED>), dim3((unsigned)(units * shape.chunks)), dim3(kThreads),
+                     lds, stream, a, shape.chunks);
   return with_keys(a.nbmax, kPickThreads, [&](auto r) {
     hipLaunchKernelGGL(pick_blocks<decltype(r)::value>, dim3(units), dim3(kPickThreads),
                        (size_t)a.lds_list * 4, stream, a);
@@ -647,6 +656,19 @@ static int row_keys(int max_seq_len, int block_shift) {
 
 size_t block_select_workspace_bytes(int units, int max_seq_len, int block_shift) {
   return (size_t)units * row_keys(max_seq_len, block_shift) * sizeof(uint32_t);
+}
+
+// (tiles hold as many rows paged as contiguous)
+LaunchSize block_select_size(const KvView& kv, int dtype, int block_shift) {
+  const int round = kWaves * (dtype == 1 ? Scorer<__bf16, 128, false>::kRows
+                              : kv.d == 128 ? Scorer<float, 128, false>::kRows
+                                            : Scorer<float, 64, false>::kRows);
+  const int nbmax = row_keys(kv.max_seq_len, block_shift);
+  const long long units = (long long)kv.batch * kv.hkv;
+  const Shape s = launch_shape(units, nbmax, (long long)nbmax * 2 * kv.d * (dtype == 1 ? 2 : 4), round);
+  if (s.one) return {units, kThreads};
+  // score_blocks; pick_blocks has twice the threads in a workgroup a row
+  return {std::max(units * s.chunks, 2 * units), kThreads};
 }
 
 hipError_t launch_block_select(const BlockSelectLaunch& s, hipStream_t stream) {

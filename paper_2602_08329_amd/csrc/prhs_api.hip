@@ -100,12 +100,12 @@ prhs_status check_blocks(const prhs_kv* kv, int32_t block_size, int* shift) {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
-// Workgroups of a launch: its threads, at most 1024 each, must stay countable
-// in 32 bits.
-prhs_status check_grid(long long groups) {
-  if (groups >= (1LL << 22))
-    return fail(PRHS_E_UNSUPPORTED, "the call would launch %lld workgroups, at most 2^22 - 1 are",
-                groups);
+// The threads of a launch must stay countable in 32 bits.
+prhs_status check_grid(const prhs::LaunchSize& size) {
+  if (size.groups >= (1LL << 32) / size.threads)
+    return fail(PRHS_E_UNSUPPORTED,
+                "the call would launch %lld workgroups of %d threads, 2^32 or more", size.groups,
+                size.threads);
   return PRHS_OK;
 }
 
@@ -419,7 +419,7 @@ static prhs_status attention_common(const prhs_kv* kv, const prhs::QuantScales* 
   const int rows_cap = dense ? kv->max_seq_len : set_cap;
   if (scales) {
     const long long groups = prhs::quant_attn_groups(kv->batch, kv->num_kv_heads, rows_cap);
-    st = check_grid(std::max((long long)kv->batch * kv->num_q_heads, groups));
+    st = check_grid({std::max((long long)kv->batch * kv->num_q_heads, groups), 1024});
     if (st != PRHS_OK) return st;
   }
   const size_t wsz =
@@ -656,19 +656,17 @@ prhs_status prhs_quant_store(const prhs_quant_kv* kv, const void* k_new, const v
                   bounds->block_size, kv->block_size);
   }
   if (new_cap < 0) return fail(PRHS_E_INVALID, "new_cap must be >= 0 (got %d)", new_cap);
-  if ((st = check_grid((long long)kv->kv.batch * kv->kv.num_kv_heads *
-                       (ceil_div(std::min(new_cap, kv->kv.max_seq_len), kv->block_size) + 1))) != PRHS_OK)
-    return st;
-  if (kv->kv.batch == 0 || new_cap == 0) return PRHS_OK;
-  if (!k_new || !v_new) return fail(PRHS_E_INVALID, "k_new and v_new must be non-NULL");
   prhs::QuantStoreLaunch a;
   a.kv = view_of(&kv->kv);
+  a.tok.lens = new_lens;
+  a.tok.cap = new_cap;
+  if ((st = check_grid(prhs::quant_store_size(a.kv, a.tok, shift))) != PRHS_OK) return st;
+  if (kv->kv.batch == 0 || new_cap == 0) return PRHS_OK;
+  if (!k_new || !v_new) return fail(PRHS_E_INVALID, "k_new and v_new must be non-NULL");
   a.dtype = kv->kv.dtype;
   a.block_shift = shift;
   a.k_new = k_new;
   a.v_new = v_new;
-  a.tok.lens = new_lens;
-  a.tok.cap = new_cap;
   a.k_scale = kv->k_scale;
   a.v_scale = kv->v_scale;
   a.k_min = bounds ? bounds->k_min : nullptr;
@@ -747,16 +745,14 @@ prhs_status prhs_block_bounds(const prhs_kv* kv, const prhs_bounds* bounds, int3
   int shift = 0;
   if ((st = check_bounds(kv, bounds, &shift)) != PRHS_OK) return st;
   if (new_cap < 0) return fail(PRHS_E_INVALID, "new_cap must be >= 0 (got %d)", new_cap);
-  if ((st = check_grid((long long)kv->batch * kv->num_kv_heads *
-                       (ceil_div(std::min(new_cap, kv->max_seq_len), bounds->block_size) + 1))) != PRHS_OK)
-    return st;
-  if (kv->batch == 0 || new_cap == 0) return PRHS_OK;
   prhs::BlockBoundsLaunch a;
   a.kv = view_of(kv);
-  a.dtype = kv->dtype;
-  a.block_shift = shift;
   a.tok.lens = new_lens;
   a.tok.cap = new_cap;
+  if ((st = check_grid(prhs::block_bounds_size(a.kv, a.tok, shift))) != PRHS_OK) return st;
+  if (kv->batch == 0 || new_cap == 0) return PRHS_OK;
+  a.dtype = kv->dtype;
+  a.block_shift = shift;
   a.k_min = bounds->k_min;
   a.k_max = bounds->k_max;
   return device_status(prhs::launch_block_bounds(a, (hipStream_t)stream), "prhs_block_bounds launch");
@@ -821,15 +817,14 @@ prhs_status prhs_block_select(const prhs_kv* kv, const void* q, const prhs_param
                                       params->window);
   if (set_cap < need || set_cap < 0)
     return fail(PRHS_E_CAPACITY, "set_cap (%d) < the set's bound (%lld)", set_cap, need);
+  prhs::BlockSelectLaunch a;
+  a.kv = view_of(kv);
+  if ((st = check_grid(prhs::block_select_size(a.kv, kv->dtype, shift))) != PRHS_OK) return st;
   const long long units = (long long)kv->batch * kv->num_kv_heads;
-  if ((st = check_grid(units * (ceil_div(kv->max_seq_len, bounds->block_size) / 16 + 1))) != PRHS_OK)
-    return st;
   const size_t wsz = prhs::block_select_workspace_bytes((int)units, kv->max_seq_len, shift);
   if (wsz > 0 && (!ws || ws_bytes < wsz))
     return fail(PRHS_E_WORKSPACE, "workspace of %zu bytes needed (got %zu)", wsz, ws_bytes);
   if (kv->batch == 0) return PRHS_OK;
-  prhs::BlockSelectLaunch a;
-  a.kv = view_of(kv);
   a.q = q;
   a.dtype = kv->dtype;
   a.block_shift = shift;

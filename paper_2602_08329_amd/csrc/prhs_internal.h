@@ -334,6 +334,12 @@ hipError_t launch_prefill(const PrefillLaunch& a, hipStream_t stream);
 
 // ---- 8-bit cache and block selection ----
 
+// Workgroups of a call's largest launch, and threads of one.
+struct LaunchSize {
+  long long groups;
+  int threads;
+};
+
 // Where a store or a bounds update finds its tokens: the last new_tokens()
 // positions of every sequence.
 struct NewTokens {
@@ -358,6 +364,7 @@ struct QuantStoreLaunch {
   void* k_min;          // or null
   void* k_max;
 };
+LaunchSize quant_store_size(const KvView& kv, const NewTokens& tok, int block_shift);
 hipError_t launch_quant_store(const QuantStoreLaunch& a, hipStream_t stream);
 
 struct BlockBoundsLaunch {
@@ -368,6 +375,7 @@ struct BlockBoundsLaunch {
   void* k_min;
   void* k_max;
 };
+LaunchSize block_bounds_size(const KvView& kv, const NewTokens& tok, int block_shift);
 hipError_t launch_block_bounds(const BlockBoundsLaunch& a, hipStream_t stream);
 
 struct BlockSelectLaunch {
@@ -387,6 +395,7 @@ struct BlockSelectLaunch {
   void* ws;
 };
 size_t block_select_workspace_bytes(int units, int max_seq_len, int block_shift);
+LaunchSize block_select_size(const KvView& kv, int dtype, int block_shift);
 hipError_t launch_block_select(const BlockSelectLaunch& a, hipStream_t stream);
 
 // Attention over the 8-bit cache: an AttnLaunch whose kv.k and kv.v are e4m3

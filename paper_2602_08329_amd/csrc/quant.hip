@@ -321,12 +321,23 @@ int touched_blocks(const KvView& kv, const NewTokens& tok, int shift) {
   return any < all ? any : all;
 }
 
-// f(W, VPT) as compile-time numbers for blocks of vec vectors of 64 x 8 elements:
-// as few waves as hold them at `most` vectors a thread, at most four.  The store
-// takes at most 4 (a 16k prompt, 8 heads of d 128, in blocks of 16 22.7 us, two or
+// Waves of a team for blocks of vec vectors of 64 x 8 elements: as few as hold them
+// at `most` vectors a thread, at most four.  The store takes at most 4 (a 16k prompt, 8 heads of d 128, in blocks of 16 22.7 us, two or
 // four waves a block 27.9 and 47.7; in blocks of 64 with four waves 22.3, two 25.2,
 // one 30), bounds, which hold less a thread, 8 (a 32k prompt in blocks of 64 with
 // two waves 14.5 us, four 15.8; in blocks of 16 as the store).
+constexpr int kStoreVectors = 4, kBoundsVectors = 8;
+constexpr int team_waves(int vec, int most) {
+  return vec <= most ? 1 : vec / most < 4 ? vec / most : 4;
+}
+
+// Workgroups of `blocks` blocks, one a team.
+long long team_groups(long long blocks, int shift, int d, int most) {
+  const int per = kThreads / 64 / team_waves((d << shift) / 512, most);
+  return (blocks + per - 1) / per;
+}
+
+// f(waves, vectors a thread) as compile-time numbers.
 template <int N>
 struct Const {
   static constexpr int value = N;
@@ -335,7 +346,7 @@ template <int D, int most, typename F>
 void with_team(int shift, F f) {
   auto of_block = [&](auto tokens) {
     constexpr int vec = decltype(tokens)::value * D / 512;
-    constexpr int W = vec <= most ? 1 : vec / most < 4 ? vec / most : 4;
+    constexpr int W = team_waves(vec, most);
     f(Const<W>(), Const<vec / W>());
   };
   switch (shift) {
@@ -349,10 +360,11 @@ void with_team(int shift, F f) {
 template <typename T, int D>
 hipError_t launch_store_typed(const QuantStoreLaunch& a, int nblk, hipStream_t stream) {
   const int blocks = a.kv.batch * a.kv.hkv * nblk;
-  with_team<D, 4>(a.block_shift, [&](auto w, auto v) {
-    constexpr int W = decltype(w)::value, V = decltype(v)::value, per = kThreads / 64 / W;
-    hipLaunchKernelGGL((quant_store<T, D, W, V>), dim3((blocks + per - 1) / per, 2), dim3(kThreads), 0,
-                       stream, a, nblk, blocks);
+  const unsigned groups = (unsigned)team_groups(blocks, a.block_shift, D, kStoreVectors);
+  with_team<D, kStoreVectors>(a.block_shift, [&](auto w, auto v) {
+    constexpr int W = decltype(w)::value, V = decltype(v)::value;
+    hipLaunchKernelGGL((quant_store<T, D, W, V>), dim3(groups, 2), dim3(kThreads), 0, stream, a, nblk,
+                       blocks);
   });
   return hipGetLastError();
 }
@@ -360,15 +372,26 @@ hipError_t launch_store_typed(const QuantStoreLaunch& a, int nblk, hipStream_t s
 template <typename T, int D>
 hipError_t launch_bounds_typed(const BlockBoundsLaunch& a, int nblk, hipStream_t stream) {
   const int blocks = a.kv.batch * a.kv.hkv * nblk;
-  with_team<D, 8>(a.block_shift, [&](auto w, auto v) {
-    constexpr int W = decltype(w)::value, V = decltype(v)::value, per = kThreads / 64 / W;
-    hipLaunchKernelGGL((block_bounds<T, D, W, V>), dim3((blocks + per - 1) / per), dim3(kThreads), 0,
-                       stream, a, nblk, blocks);
+  const unsigned groups = (unsigned)team_groups(blocks, a.block_shift, D, kBoundsVectors);
+  with_team<D, kBoundsVectors>(a.block_shift, [&](auto w, auto v) {
+    constexpr int W = decltype(w)::value, V = decltype(v)::value;
+    hipLaunchKernelGGL((block_bounds<T, D, W, V>), dim3(groups), dim3(kThreads), 0, stream, a, nblk,
+                       blocks);
   });
   return hipGetLastError();
 }
 
 }  // namespace
+
+LaunchSize quant_store_size(const KvView& kv, const NewTokens& tok, int block_shift) {
+  const long long blocks = (long long)kv.batch * kv.hkv * touched_blocks(kv, tok, block_shift);
+  return {2 * team_groups(blocks, block_shift, kv.d, kStoreVectors), kThreads};
+}
+
+LaunchSize block_bounds_size(const KvView& kv, const NewTokens& tok, int block_shift) {
+  const long long blocks = (long long)kv.batch * kv.hkv * touched_blocks(kv, tok, block_shift);
+  return {team_groups(blocks, block_shift, kv.d, kBoundsVectors), kThreads};
+}
 
 hipError_t launch_quant_store(const QuantStoreLaunch& a, hipStream_t stream) {
   const int nblk = touched_blocks(a.kv, a.tok, a.block_shift);
