@@ -373,7 +373,7 @@ class QuantKV:
             raise ValueError("dtype must be float32 or bfloat16")
         _need(K8, torch.float8_e4m3fn, "K8", dims=4)
         _need(V8, torch.float8_e4m3fn, "V8", shape=K8.shape)
-        _need(k_scale, torch.float32, "k_scale")
+        _need(k_scale, torch.float32, "k_scale", dims=3 if block_table is None else 2)
         _need(v_scale, torch.float32, "v_scale", shape=k_scale.shape)
         _need(seq_lens, torch.int32, "seq_lens", dims=1)
         if block_table is not None:
