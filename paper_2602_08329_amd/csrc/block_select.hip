@@ -654,7 +654,7 @@ static int row_keys(int max_seq_len, int block_shift) {
   return (((max_seq_len + (1 << block_shift) - 1) >> block_shift) + kKeys - 1) / kKeys * kKeys;
 }
 
-size_t block_select_workspace_bytes(int units, int max_seq_len, int block_shift) {
+size_t block_select_workspace_bytes(long long units, int max_seq_len, int block_shift) {
   return (size_t)units * row_keys(max_seq_len, block_shift) * sizeof(uint32_t);
 }
 

@@ -789,7 +789,8 @@ prhs_status prhs_block_workspace_size(const prhs_kv* kv, const prhs_bounds* boun
   if (!bounds) return fail(PRHS_E_INVALID, "bounds is NULL");
   int shift = 0;
   if ((st = check_blocks(kv, bounds->block_size, &shift)) != PRHS_OK) return st;
-  *bytes = prhs::block_select_workspace_bytes(kv->batch * kv->num_kv_heads, kv->max_seq_len, shift);
+  *bytes = prhs::block_select_workspace_bytes((long long)kv->batch * kv->num_kv_heads, kv->max_seq_len,
+                                              shift);
   return PRHS_OK;
 }
 
@@ -821,7 +822,7 @@ prhs_status prhs_block_select(const prhs_kv* kv, const void* q, const prhs_param
   a.kv = view_of(kv);
   if ((st = check_grid(prhs::block_select_size(a.kv, kv->dtype, shift))) != PRHS_OK) return st;
   const long long units = (long long)kv->batch * kv->num_kv_heads;
-  const size_t wsz = prhs::block_select_workspace_bytes((int)units, kv->max_seq_len, shift);
+  const size_t wsz = prhs::block_select_workspace_bytes(units, kv->max_seq_len, shift);
   if (wsz > 0 && (!ws || ws_bytes < wsz))
     return fail(PRHS_E_WORKSPACE, "workspace of %zu bytes needed (got %zu)", wsz, ws_bytes);
   if (kv->batch == 0) return PRHS_OK;

@@ -394,7 +394,7 @@ struct BlockSelectLaunch {
   int set_cap;
   void* ws;
 };
-size_t block_select_workspace_bytes(int units, int max_seq_len, int block_shift);
+size_t block_select_workspace_bytes(long long units, int max_seq_len, int block_shift);
 LaunchSize block_select_size(const KvView& kv, int dtype, int block_shift);
 hipError_t launch_block_select(const BlockSelectLaunch& a, hipStream_t stream);
 
