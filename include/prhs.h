@@ -503,8 +503,9 @@ prhs_status prhs_pool_decode_attn(const prhs_kv* kv, const void* q, const int32_
  * block holds earlier tokens, from its present bounds.
  * k_new, v_new: [batch][num_kv_heads][new_cap][head_dim] in kv->kv.dtype;
  * new_lens: [batch] int32 device array or NULL.
- * Two sequences whose block tables name one page must not both store into it
- * in one call (its contents are then unspecified).  Tokens on pages outside
+ * No page is stored into twice in one call, by two sequences whose block
+ * tables name it or by one that names it twice (its contents are then
+ * unspecified).  Tokens on pages outside
  * the pool are dropped.  No workspace. */
 prhs_status prhs_quant_store(const prhs_quant_kv* kv, const void* k_new, const void* v_new,
                              int32_t new_cap, const int32_t* new_lens, const prhs_bounds* bounds,

@@ -3,11 +3,11 @@
 //   sum_d max(q kmin, q kmax) = q+ . kmax + q- . kmin,
 // an upper bound of q . k over the keys that the bounds were made of (for an 8-bit
 // cache those given to the store, which rounds them to 4 bits): a product of length
-// 2d, on MFMA for bf16 and in vector fp32 for fp32 bounds.  What bounds it is reading the
-// bounds (4d bytes a block in bf16) once: 512 rows of 4096 blocks at d 128 (1.07
-// GB) 181 us, 5.9 TB/s, where a kernel that only loads them in the same order
-// takes 150.  The scoring without its arithmetic takes the same time; the pick
-// costs a row of 8192 blocks 8 us in a launch of its own.
+// 2d, on MFMA for bf16 and in vector fp32 for fp32 bounds.  What bounds it is
+// reading the bounds (4d bytes a block in bf16) once: 512 rows of 4096 blocks at d
+// 128 (1.07 GB) 181 us, 5.9 TB/s, where a kernel that only loads them in the same
+// order takes 150.  The scoring without its arithmetic takes the same time; the pick
+// costs a row of 8192 blocks 7.5 us in a launch of its own.
 //
 // Scores become order-preserving keys (0, below every number's key, for NaN and
 // for blocks whose page lies outside the pool).  The key of the last chosen block
@@ -564,7 +564,8 @@ __global__ __launch_bounds__(kThreads) void select_blocks(BlockArgs a) {
 // and 107, 512 of 512 KB 52.8 and 59.1, ragged 42.1 and 48.1; 256 of 8 MB 404 and
 // 384), but for long rows of a few more units than CUs, which wait for the CUs that
 // take two (264 of 512 KB 37.5 and 35.1, 320 of 2 MB 143 and 125; 384 of 512 KB 43.2
-// and 46.1, of 2 MB 150 and 148).
+// and 46.1, of 2 MB 150 and 148).  The CUs are those of a whole chip; on a part of one
+// both forms are as right, but not the faster one is always taken.
 bool one_launch(long long units, long long row_bytes) {
   constexpr long long KB = 1024;
   if (row_bytes <= 192 * KB) return true;

@@ -15,9 +15,9 @@
 // A team reads its new elements once, 8 per thread and step, holds them in
 // registers while their maximum is taken, and writes their bytes.  Bounds come
 // from the same registers.  Moving the bytes bounds both kernels: a 16k prompt of
-// 8 heads of d 128 in bf16 (67 MB read, 38 written) is stored in 22.7 us, 4.6 TB/s
+// 8 heads of d 128 in bf16 (67 MB read, 38 written) is stored in 22.8 us, 4.6 TB/s
 // where a large copy reaches 4.9, the bounds of a 32k prompt (67 MB, 2 written)
-// take 14.5, 4.8 TB/s; a step of 64 sequences takes 5.0 and 4.5, the time of a
+// take 12.8, 5.4 TB/s; a step of 64 sequences takes 5.0 and 4.9, the time of a
 // launch whose loads of lengths, pages and tokens follow each other.
 #include "prhs_internal.h"
 
@@ -322,10 +322,11 @@ int touched_blocks(const KvView& kv, const NewTokens& tok, int shift) {
 }
 
 // Waves of a team for blocks of vec vectors of 64 x 8 elements: as few as hold them
-// at `most` vectors a thread, at most four.  The store takes at most 4 (a 16k prompt, 8 heads of d 128, in blocks of 16 22.7 us, two or
-// four waves a block 27.9 and 47.7; in blocks of 64 with four waves 22.3, two 25.2,
-// one 30), bounds, which hold less a thread, 8 (a 32k prompt in blocks of 64 with
-// two waves 14.5 us, four 15.8; in blocks of 16 as the store).
+// at `most` vectors a thread, at most four.  Replayed graphs, 8 heads of d 128 in
+// bf16: the store takes at most 4 (a 16k prompt in blocks of 16 20.8 us, two or four
+// waves a block 25.2 and 43.5; in blocks of 64 with four waves 20.9, two 23.6, one
+// 28.6), bounds, which hold less a thread, 8 (a 32k prompt in blocks of 64 with two
+// waves 13.3 us, four 14.1; in blocks of 16 as the store).
 constexpr int kStoreVectors = 4, kBoundsVectors = 8;
 constexpr int team_waves(int vec, int most) {
   return vec <= most ? 1 : vec / most < 4 ? vec / most : 4;

@@ -26,11 +26,11 @@
 // behind a branch would make the compiler wait for all of them.
 //
 // Reading the bytes bounds long streams: 64 sequences of 8k to 16k, 32 over 8
-// heads of d 128 (1.59 GB) 243 us, 6.5 TB/s, 8 of 4k with 32 kv heads (269 MB) 42
+// heads of d 128 (1.59 GB) 242 us, 6.6 TB/s, 8 of 4k with 32 kv heads (269 MB) 42
 // us, 6.4 TB/s, where a plain read reaches 7.1.  Few units are bound by the chain of
 // loads (list, page, row), the joining of the waves and the second launch: the
-// selected set of one 128k sequence (8 units of 2300 rows, 4.8 MB) 7.1 us and 3.5 in
-// attn_merge.
+// selected set of one 128k sequence (8 units of 2300 rows, 4.8 MB) 10.6 us, in a
+// trace 7.8 and 4.0 in attn_merge.
 #include <algorithm>
 #include <cmath>
 
@@ -486,23 +486,25 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_attn_split(QuantArgs a) 
   }
 }
 
-// Splits of a unit and rows of a split, a multiple of the tile.  Times in us, d 128
-// with 4 heads a kv head where nothing else is said.
+// Splits of a unit and rows of a split, a multiple of the tile.  Times in us of
+// replayed graphs, d 128 with 4 heads a kv head where nothing else is said.
 // Up to 256 units: one workgroup of eight waves a CU (64 units of ragged 16384 rows
-// 38.9, two of four waves 43.9), two where that fills the CUs better (96 units of
-// ragged 16384 rows in two 60.8, in five 56.0; 72 of 1600 in three 14.2, in seven
-// 13.8), but no more splits than is worth their joining, each 0.05 (one unit of
-// 32768 rows in 256 22.3, in 64 14.4, of 131072 26.1, in 128 21.3), so that their
+// 35.2, two of four waves 44.5), two where that fills the CUs better (96 units of
+// ragged 16384 rows in two 54.8, in five 51.3; 72 of 1600 in three 12.7, in seven
+// 12.4), but no more splits than is worth their joining, each 0.05 (one unit of
+// 32768 rows in 256 20.5, in 64 13.0, of 131072 24.6, in 128 19.6), so that their
 // number grows with the root of the rows.  No split of few rows, which saves the
-// merge launch (8 units of 600 rows 9.6 whole, 11.0 in four; of 1000 11.8 and 11.1;
-// 96 units of 1600 rows 16.2 whole, 15.4 in five, as sets 17.0 and 17.1; 120 16.3
-// and 16.9), no split below kMinSplit rows, and of more than 128 units only long
-// ones (136 of 12000 rows 79.0 whole, 73.5 in three, of ragged 16384 92.8 and 78.9;
-// 160 of 4096 31.4 and 34.3).
+// merge launch (8 units of 600 rows 8.1 whole, 9.0 in four; of 1000 10.4 and 9.2;
+// 96 units of 1600 rows 14.0 whole, 13.8 in five; 120 14.2 and 15.3), no split below
+// kMinSplit rows, and of more than 128 units only long ones (136 of 12000 rows 76.2
+// whole, 70.6 in three, of ragged 16384 92.0 and 78.4; 160 of 4096 29.7 and 32.9).
 // More units than CUs: whole, as the workgroups of a CU share it (512 of 16384 rows
-// 326, in two 334), but long rows of a few more units than CUs, which wait for the
-// CUs that take two (264 of 4096 rows 61.4 whole, 54.7 in four; 320 of 16384 244
-// and 215; 384 of 16384 262 and 255).
+// 318, in two 325), but long rows of a few more units than CUs, which wait for the
+// CUs that take two (264 of 4096 rows 55.5 whole, 53.8 in four; 320 of 16384 251
+// and 207; 384 of 16384 255 and 247).
+// The CUs are those of a whole chip, a number and no question to the device, since
+// workspaces are sized by it where there is none; on a part of a chip the splits are
+// as right, but not the fastest.
 constexpr long long kCus = 256;
 constexpr int kWholeFew = 850, kWholeMany = 1536, kFewUnits = 64;
 constexpr int kMinSplit = 128;
@@ -527,12 +529,12 @@ void split_geometry(long long units, int rows_cap, int* chunk, int* nsplit) {
 }
 
 // Waves of a workgroup, one for each tile at most: eight where it has a CU to
-// itself (256 units of 600 rows 13.1, with four 13.3, with two 16.5) and for long
-// streams (64 ragged sequences of up to 16384 rows, 8 kv heads, in length order 248
-// us, with four 264, of equal lengths 331 and 330), else four (512 of 600 rows 20.0,
-// with eight 22.6).  Short streams of many heads take waves for joining the heads'
-// rows too (64 units of 16 heads and 7 rows 7.3 with four waves, 10.2 with one; 512
-// of 4 heads and 64 rows 7.4 with their two, 7.9 with four).
+// itself (256 units of 600 rows 11.0, with four 11.5, with two 14.2) and for long
+// streams (64 ragged sequences of up to 16384 rows, 8 kv heads, in length order 238
+// us, with four 252, of equal lengths 317 and 315), else four (512 of 600 rows 18.6,
+// with eight 19.9).  Short streams of many heads take waves for joining the heads'
+// rows too (64 units of 16 heads and 7 rows 5.4 with four waves, 8.4 with one; 512
+// of 4 heads and 64 rows 6.0 with their two, 6.4 with four).
 int waves_for(long long groups, int chunk, int outputs) {
   const int most = groups <= kCus || chunk > 8192 ? kMaxWaves : 4;
   return std::min(most, std::max(chunk / kTile, std::min(4, outputs / 512)));
@@ -543,8 +545,8 @@ hipError_t launch_typed(QuantArgs& a, hipStream_t stream) {
   const int units = a.kv.batch * a.kv.hkv, G = a.kv.hq / a.kv.hkv;
   const int waves = waves_for((long long)units * a.nsplit, a.chunk, G * D);
   // long whole streams on more units than CUs, which take another as they end
-  // (64 ragged sequences of 8k to 16k, 8 kv heads: 260 us in index order, 248; of
-  // equal lengths 326 and 331)
+  // (64 ragged sequences of 8k to 16k, 8 kv heads: 246 us in index order, 238; of
+  // equal lengths 313 and 317)
   a.by_length = DENSE && a.nsplit == 1 && units > kCus && a.chunk > 8192 && a.kv.batch > 1 && a.kv.batch <= 1024;
   const size_t dyn = (size_t)waves * wave_bytes(D, G) + query_bytes(D, QP);
   if (dyn > 49152) {
