@@ -481,8 +481,9 @@ prhs_status prhs_pool_decode_attn(const prhs_kv* kv, const void* q, const int32_
  * prhs_quant_store writes tokens into it, the prhs_quant_*_decode_attn calls
  * attend it as their namesakes attend a bf16 or fp32 cache.  A call of this
  * section or the next whose launch would have 2^32 threads or more returns
- * PRHS_E_UNSUPPORTED: stores and bounds beyond about 2^24 blocks, selections
- * beyond 2^22 rows, attention from 2^22 (batch x num_q_heads) on. */
+ * PRHS_E_UNSUPPORTED.  That takes a store 2^23 blocks at least (2^25 of 16
+ * tokens), bounds 2^24 and a selection 2^22 rows; attention is refused from
+ * batch x num_q_heads = 2^22 on. */
 
 /* Stores new keys and values.  For every sequence b with n = seq_lens[b] and
  * c = min(new_lens[b], new_cap, n) (new_lens NULL: c = min(new_cap, n)), the
