@@ -8,11 +8,12 @@
 // an operand to less than fp32 holds: K with q (fp32 queries as three bf16 parts,
 // 24 bits), V with the weights w_i = p_i vs_i r, three bf16 parts as well, r a
 // power of two, at most 2^126, that brings the largest vs the wave has met to
-// [2^80, 2^81) (a normal one to 1 or more).  p stays below 2^8 (lazy rescaling), so
+// [2^80, 2^81) (a normal one to 1 or more).  p is at most 2^8 (lazy rescaling), so
 // sums over 2^22 rows stay below 2^120, and the parts are normal numbers for w down
-// to 2^-110, which the largest weight exceeds 2^110 times at least.  (Two fp16 parts have too little range: beside a block whose
-// values are 2^20 times the others' they left about ten bits of the others' weights.
-// They cost a product less: one sequence of 617 tokens 8.8 us, 9.3 so.)
+// to 2^-110, at most that part of the largest weight.  Two fp16 parts have too
+// little range: beside a block whose values are 2^20 times the others' they left
+// about ten bits of the others' weights.  They cost a product less: one sequence of
+// 617 tokens 8.8 us, 9.3 so.
 // With at most 8 heads a kv head, two of the parts are two columns of one product
 // (the queries stand in the columns twice), else each part is a product.
 //
